@@ -312,6 +312,144 @@ const char* dkv_strerror(int code);
 /* Library version, 1000*major + minor. */
 int dkv_version(void);
 
+/* ---- Generation after a compressed prompt --------------------------------------------------------------------
+ * The buffers above end where the prompt ends.  Below is what generation goes on in: a cache of pages that holds keys
+ * and values in 8 bits, which a compressed prompt moves into, to which decoded tokens are added, and whose pages return to
+ * a pool that all layers and samples share (after compression every layer has another length); and the rotary positions
+ * that queries and keys have before they are scored, cached or attended to. */
+
+/* A tensor [batch][heads][tokens][head_dim] in device memory: strides in elements, not negative; a head's dims lie side by
+ * side.  type: DKV_BF16, DKV_F16, DKV_F32, or DKV_RAW16 for 16-bit patterns of whatever type the cache was made for. */
+#define DKV_BF16  0
+#define DKV_F16   1
+#define DKV_F32   2
+#define DKV_RAW16 3
+typedef struct {
+  void* data;
+  int32_t type, batch, heads, tokens, head_dim;
+  int64_t batch_stride, head_stride, token_stride;
+} dkv_rows;
+
+/* Rotary positions: of a head's first rot_dim dims every pair (a, b) is turned by t = position * f_i,
+ *   (a, b) -> A (a cos t - b sin t, a sin t + b cos t),   i = 0 .. rot_dim/2 - 1,
+ * the other dims stay.  Without scaling f_i = theta^(-2i/rot_dim) and A = 1. */
+#define DKV_ROTARY_HALF   0   /* pairs (i, i + rot_dim/2) */
+#define DKV_ROTARY_PAIRS  1   /* pairs (2i, 2i+1)         */
+#define DKV_SCALING_NONE       0
+#define DKV_SCALING_LINEAR     1   /* f_i / factor                                                                       */
+#define DKV_SCALING_BASE       2   /* theta * factor^(rot_dim/(rot_dim-2)) in place of theta (rot_dim > 2)               */
+#define DKV_SCALING_WAVELENGTH 3   /* w = trained_len * f_i / (2 pi) turns; f_i / factor for w <= low, f_i for w >= high,
+                                      between them the blend f_i / factor * (1-b) + f_i * b, b = (w-low)/(high-low)      */
+#define DKV_SCALING_RAMP       4   /* f_i / factor * r + f_i * (1-r), r = clamp((i-x)/(y-x), 0, 1) with x = floor, y = ceil of
+                                      the i at which a pair makes `high` (x) and `low` (y) turns in trained_len positions,
+                                      kept inside 0 .. rot_dim-1; A = 0.1 ln(factor) + 1                                */
+typedef struct {
+  int32_t head_dim;        /* even, 2..256                                         */
+  int32_t rot_dim;         /* even, 2..head_dim                                    */
+  int32_t layout;          /* DKV_ROTARY_*                                         */
+  int32_t scaling;         /* DKV_SCALING_*                                        */
+  double theta;            /* > 0                                                  */
+  double factor;           /* >= 1; unused without scaling                         */
+  double low, high;        /* 0 < low < high; WAVELENGTH and RAMP                  */
+  double trained_len;      /* > 0; WAVELENGTH and RAMP                             */
+} dkv_rotary_config;
+/* What the calls take: filled once by dkv_rotary_init, owned and kept by the caller (plain data, no device memory). */
+typedef struct {
+  int32_t head_dim, rot_dim, layout;
+  float amplitude;         /* A                                                    */
+  double turns[128];       /* f_i / (2 pi)                                         */
+} dkv_rotary;
+/* Host call.  Errors: INVALID_ARG. */
+int dkv_rotary_init(const dkv_rotary_config* cfg, dkv_rotary* out);
+/* Turn x into x_out, and y into y_out where y is given (queries and keys of one call; same batch, tokens, head_dim and type).
+ *   pos : int32 [batch][tokens], device: positions, of any size or sign.  Angles are reduced in 64 bits.
+ *   transpose != 0: the gradient, i.e. sin negated: given d/d x_out it writes d/d x.
+ * fp32 arithmetic, one rounding.  x_out may be x itself (same strides); no other overlap, and no element of an output twice.
+ * Errors: INVALID_ARG (also a type DKV_RAW16, or data not aligned to its element).  The call may be captured into a CUDA graph. */
+int dkv_rotate(const dkv_rotary* r, const int32_t* pos, const dkv_rows* x, const dkv_rows* x_out, const dkv_rows* y,
+               const dkv_rows* y_out, int32_t transpose, void* stream);
+
+/* The cache.  n_seqs sequences share n_pages pages; a page holds page_rows rows of every KV head of one sequence.  A program
+ * with L layers and Bt samples makes L*Bt sequences, for instance number layer*Bt + sample: every call names sequences
+ * first, first + step, .., n of them, so step 1 is a layer and step Bt is a sample.
+ * Per page, KV head and tensor (K, V) there is one scale, a power of two not below 2^-126: value = code * scale.  Codes are
+ * numbers e4m3 (largest 448) or int8 (largest 127), rounded to the nearest (ties to even).  The scale of a page is the
+ * smallest that its rows needed when they were added; a row added later may raise it, and the page's older codes are then
+ * rounded again (no change for e4m3 but for what becomes subnormal).  Infinities are stored as the largest code of their
+ * page and NaN as 0, so that no row can spoil a query that does not see it; dkv_cache8_status tells that there were some. */
+#define DKV_E4M3 0
+#define DKV_INT8 1
+typedef struct {
+  int32_t n_pages;         /* 1 .. 2^26                                            */
+  int32_t page_rows;       /* R: 32, 64 or 128                                     */
+  int32_t n_seqs;          /* 1 .. 65535                                           */
+  int32_t max_pages;       /* pages a sequence can hold; max_pages * R <= 2^24     */
+  int32_t n_q_heads;       /* multiple of n_kv_heads                               */
+  int32_t n_kv_heads;      /* 1 .. 32767                                           */
+  int32_t head_dim;        /* 64 or 128                                            */
+  int32_t kind;            /* DKV_E4M3 or DKV_INT8                                 */
+  int32_t io;              /* DKV_BF16 or DKV_F16: rows and queries                */
+} dkv_cache8_config;
+typedef struct dkv_cache8 dkv_cache8;
+
+/* Create a cache without rows on the current device (host call; allocates n_pages * 2 * n_kv_heads * (R * head_dim + 4) bytes of pages,
+ * 8 * n_seqs * max_pages of tables and, for dkv_cache8_attend, about 68 KB an SM).  It belongs to that device and to one stream at
+ * a time: calls on it, replays of graphs that hold such calls included, follow one another.
+ * Errors: INVALID_ARG, UNSUPPORTED, NOMEM, CUDA.  On error *out is NULL. */
+int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out);
+/* Free everything (synchronises the device). */
+int dkv_cache8_destroy(dkv_cache8* c);
+
+/* All calls below: INVALID_ARG for sequences that do not exist, shapes or types that are not the cache's, data not 16-byte
+ * aligned or strides that are no multiple of 8 elements, or when another device than the cache's is current.  n = 0 does
+ * nothing.  What the device decides (lengths, pages) is reported by dkv_cache8_status; no call reads or writes out of bounds. */
+
+/* Room for rows[i] more rows of the i-th sequence (rows: int32 [n], device; NULL: `add` each).  The lowest free pages are given
+ * out in the order of the sequences.  Where pages do not last, the first sequence that cannot be served and all after it in
+ * this call get none.  A sequence whose last page is partly filled and shared with a fork gets its own copy of it.  Rows
+ * reserved earlier and not yet added count. */
+int dkv_cache8_reserve(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* rows, int32_t add, void* stream);
+/* The first rows[i] of k[i], v[i] ([n, n_kv_heads, tokens, head_dim]) go behind the rows of the i-th sequence
+ * (rows: int32 [n], device, at most `tokens`; NULL: all).  With `rotary` the keys are turned first, row j by position
+ * pos0[i] + j (int32 [n], device), without a rounding in between; both are NULL otherwise.  A sequence without room (dkv_cache8_reserve
+ * comes first, and again after a fork) stays as it is and is reported.  A prompt's compressed buffers move in with kb, vb and the
+ * lengths that dkv_compact reports. */
+int dkv_cache8_append(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const dkv_rows* k, const dkv_rows* v, const int32_t* rows,
+                      const dkv_rotary* rotary, const int32_t* pos0, void* stream);
+/* The rows as 16-bit numbers: row j of the i-th sequence to k_out[i, :, j], v_out[i, :, j], j < tokens; rows past the
+ * sequence's length are not written.  What exceeds the 16-bit type becomes its largest number. */
+int dkv_cache8_read(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const dkv_rows* k_out, const dkv_rows* v_out, void* stream);
+/* Attention of tokens = nq new queries a sequence, q [n, n_q_heads, nq, head_dim], over the sequence's rows:
+ *   out = softmax(q . K^T / sqrt(head_dim)) V,  fp32 [n, n_q_heads, nq, head_dim];
+ *   lse : fp32 [n, n_q_heads, nq], the natural logarithm of the denominators (NULL: not wanted).
+ * causal != 0: the queries are those of the last nq rows, query j sees all rows but the last nq-1-j.  A query that sees no row
+ * gets 0 and -infinity.  n_q_heads / n_kv_heads * nq <= 64.  Deterministic. */
+int dkv_cache8_attend(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const dkv_rows* q, const dkv_rows* out, float* lse,
+                      int32_t causal, void* stream);
+/* Sequences to, to + step, .. become forks of from, from + step, ..: what they held is given back, and they share the source's
+ * pages.  No sequence may be source and fork in one call (INVALID_ARG).  Either side may then be appended to, after a
+ * dkv_cache8_reserve that gives it its own copy of a last page that is partly filled. */
+int dkv_cache8_fork(dkv_cache8* c, int32_t from, int32_t to, int32_t n, int32_t step, void* stream);
+/* Every KV head h keeps rows idx[i][h][0 .. count[i]) of the i-th sequence, in that order (idx: int32 [n, heads, cols], heads = n_kv_heads,
+ * count: int32 [n] or NULL: cols each; device).  They move to new pages, whose scales are those that the kept values need, and
+ * the old pages are given back: until then both are held, so free pages for the kept rows must be there (else the sequence
+ * stays as it is, and is reported).  A row number outside the sequence is reported and gives a row of zeros. */
+int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* idx, int32_t heads, int32_t cols,
+                       const int32_t* count, void* stream);
+/* Cut sequences to keep[i] rows (int32 [n], device; more than there are: no cut), or where keep is NULL by `drop` >= 0 rows
+ * (as far as there are).  Pages behind the last row are given back, reserved ones too: drop = INT32_MAX frees a sequence. */
+int dkv_cache8_trim(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* keep, int32_t drop, void* stream);
+/* Device-side views, owned by the cache (any may be NULL): len int32 [n_seqs] rows, held int32 [n_seqs] pages, table int32
+ * [n_seqs][max_pages] (the first held entries of each), refs int32 [n_pages] sequences that hold a page. */
+int dkv_cache8_views(dkv_cache8* c, const int32_t** len, const int32_t** held, const int32_t** table, const int32_t** refs);
+/* Synchronises the device.  host int32 [8]: [0] what went wrong since the last report, as bits: 1 no free pages, 2 more pages than a
+ * sequence's table holds, 4 rows added without room, 8 a count or row number out of range, 16 an infinity or NaN was stored;
+ * [1] the lowest sequence concerned (-1: none), [2] free pages now, [3] low and [4] high half of the kernels launched.
+ * Returns DKV_OK, DKV_ERR_NOMEM for bits 1 or 2, else DKV_ERR_STATE for bit 4, else DKV_ERR_INVALID_ARG for bit 8. */
+int dkv_cache8_status(dkv_cache8* c, int32_t* host_status);
+/* CUDA error code of the last DKV_ERR_CUDA on this cache (0 = none). */
+int dkv_cache8_last_cuda_error(dkv_cache8* c);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,7 +23,9 @@ EXPORTS = [
     "dkv_apply_policy", "dkv_select_positions", "dkv_decode_attend", "dkv_get_counts",
     "dkv_layer_views", "dkv_kept_sorted", "dkv_budget_views", "dkv_memcpy_to_host", "dkv_last_status",
     "dkv_static_last_status", "dkv_set_wait_limit", "dkv_debug_withhold_tile", "dkv_profile", "dkv_profile_read", "dkv_launch_count", "dkv_last_cuda_error",
-    "dkv_strerror", "dkv_version",
+    "dkv_strerror", "dkv_version", "dkv_rotary_init", "dkv_rotate", "dkv_cache8_create", "dkv_cache8_destroy", "dkv_cache8_reserve",
+    "dkv_cache8_append", "dkv_cache8_read", "dkv_cache8_attend", "dkv_cache8_fork", "dkv_cache8_compact", "dkv_cache8_trim",
+    "dkv_cache8_views", "dkv_cache8_status", "dkv_cache8_last_cuda_error",
 ]
 
 DKV_OK, DKV_ERR_INVALID_ARG, DKV_ERR_STATE, DKV_ERR_CUDA = 0, -1, -2, -3
@@ -34,6 +36,27 @@ class DkvConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "n_layers", "n_q_heads", "n_kv_heads", "head_dim", "batch", "seq_len", "window", "pool_kernel",
         "pool_kind", "avg_budget", "layer_max", "update_interval")] + [("flags", ctypes.c_uint32)]
+
+
+class DkvRows(ctypes.Structure):
+    """dkv_rows, for programs without torch; with torch the calls take tensors [batch, heads, tokens, head_dim]."""
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("type", "batch", "heads", "tokens", "head_dim")] + [
+        (n, ctypes.c_int64) for n in ("batch_stride", "head_stride", "token_stride")]
+
+
+class DkvRotaryConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rot_dim", "layout", "scaling")] + [
+        (n, ctypes.c_double) for n in ("theta", "factor", "low", "high", "trained_len")]
+
+
+class DkvRotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rot_dim", "layout")] + [("amplitude", ctypes.c_float),
+                                                                                ("turns", ctypes.c_double * 128)]
+
+
+class DkvCache8Config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_rows", "n_seqs", "max_pages", "n_q_heads", "n_kv_heads",
+                                              "head_dim", "kind", "io")]
 
 
 class DkvError(RuntimeError):
@@ -90,6 +113,20 @@ def load() -> ctypes.CDLL:
         "dkv_strerror": [ctypes.c_int],
         "dkv_version": [],
         "dkv_launch_count": [vp],
+        "dkv_rotary_init": [vp, vp],
+        "dkv_rotate": [vp, vp, vp, vp, vp, vp, i32, vp],
+        "dkv_cache8_create": [ctypes.POINTER(DkvCache8Config), pp],
+        "dkv_cache8_destroy": [vp],
+        "dkv_cache8_reserve": [vp, i32, i32, i32, vp, i32, vp],
+        "dkv_cache8_append": [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp],
+        "dkv_cache8_read": [vp, i32, i32, i32, vp, vp, vp],
+        "dkv_cache8_attend": [vp, i32, i32, i32, vp, vp, vp, i32, vp],
+        "dkv_cache8_fork": [vp, i32, i32, i32, i32, vp],
+        "dkv_cache8_compact": [vp, i32, i32, i32, vp, i32, i32, vp, vp],
+        "dkv_cache8_trim": [vp, i32, i32, i32, vp, i32, vp],
+        "dkv_cache8_views": [vp, pp, pp, pp, pp],
+        "dkv_cache8_status": [vp, vp],
+        "dkv_cache8_last_cuda_error": [vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -165,6 +202,8 @@ def _ptr(x) -> Optional[int]:
         return x.ctypes.data
     if hasattr(x, "cuda_stream"):
         return x.cuda_stream
+    if isinstance(x, ctypes.Structure):
+        return ctypes.addressof(x)
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
@@ -356,3 +395,98 @@ def dkv_launch_count(ctx: int) -> int:
 
 def dkv_last_cuda_error(ctx: int) -> int:
     return load().dkv_last_cuda_error(ctx)
+
+
+# ---- generation after a compressed prompt: rotary positions and the cache in 8 bits (see include/dkv.h) ---------------
+DKV_BF16, DKV_F16, DKV_F32, DKV_RAW16 = 0, 1, 2, 3
+DKV_ROTARY_HALF, DKV_ROTARY_PAIRS = 0, 1
+DKV_SCALING_NONE, DKV_SCALING_LINEAR, DKV_SCALING_BASE, DKV_SCALING_WAVELENGTH, DKV_SCALING_RAMP = 0, 1, 2, 3, 4
+DKV_E4M3, DKV_INT8 = 0, 1
+#: Bits of dkv_cache8_status's first word.
+DKV_C8_NO_PAGES, DKV_C8_TABLE_FULL, DKV_C8_NO_ROOM, DKV_C8_BAD_ARGUMENT, DKV_C8_NOT_FINITE = 1, 2, 4, 8, 16
+
+
+def _struct(x):
+    """The address of a structure; anything else as it is."""
+    return ctypes.addressof(x) if isinstance(x, ctypes.Structure) else x
+
+
+def dkv_rotary_init(head_dim: int, rot_dim: int, layout: int, theta: float, scaling: int = DKV_SCALING_NONE, factor: float = 1.0,
+                    low: float = 1.0, high: float = 4.0, trained_len: float = 8192.0) -> DkvRotary:
+    """Frequencies of rotary positions, for dkv_rotate and dkv_cache8_append."""
+    cfg, out = DkvRotaryConfig(head_dim, rot_dim, layout, scaling, theta, factor, low, high, trained_len), DkvRotary()
+    _check(load().dkv_rotary_init(ctypes.addressof(cfg), ctypes.addressof(out)), "dkv_rotary_init")
+    return out
+
+
+def dkv_rotate(rotary: DkvRotary, pos, x, x_out, y=None, y_out=None, transpose=False, stream=None) -> None:
+    """Turn x [batch, heads, tokens, head_dim] by the positions int32 [batch, tokens], and y with it; transpose: the gradient."""
+    _check(_native().rotate(_struct(rotary), pos, _struct(x), _struct(x_out), _struct(y), _struct(y_out), transpose, stream), "dkv_rotate")
+
+
+def make_cache8_config(n_pages, page_rows, n_seqs, max_pages, n_q_heads, n_kv_heads, head_dim, kind=DKV_E4M3, io=DKV_BF16) -> DkvCache8Config:
+    return DkvCache8Config(n_pages, page_rows, n_seqs, max_pages, n_q_heads, n_kv_heads, head_dim, kind, io)
+
+
+def dkv_cache8_create(cfg: DkvCache8Config) -> int:
+    h = ctypes.c_void_p()
+    _check(load().dkv_cache8_create(ctypes.byref(cfg), ctypes.byref(h)), "dkv_cache8_create")
+    return h.value
+
+
+def dkv_cache8_destroy(cache: int) -> None:
+    _check(load().dkv_cache8_destroy(cache), "dkv_cache8_destroy")
+
+
+def dkv_cache8_reserve(cache: int, first: int, n: int, step: int, rows=None, add: int = 0, stream=None) -> None:
+    """Room for rows[i] (int32 [n], device) or `add` more rows of sequences first, first + step, .."""
+    _check(_native().cache8_reserve(cache, first, n, step, rows, add, stream), "dkv_cache8_reserve")
+
+
+def dkv_cache8_append(cache: int, first: int, n: int, step: int, k, v, rows=None, rotary: Optional[DkvRotary] = None, pos0=None,
+                      stream=None) -> None:
+    """Add the first rows[i] rows of k[i], v[i] [n, n_kv_heads, tokens, head_dim], the keys turned from position pos0[i] on."""
+    _check(_native().cache8_append(cache, first, n, step, _struct(k), _struct(v), rows, _struct(rotary), pos0, stream), "dkv_cache8_append")
+
+
+def dkv_cache8_read(cache: int, first: int, n: int, step: int, k_out, v_out, stream=None) -> None:
+    """The sequences' rows as 16-bit numbers into k_out, v_out [n, n_kv_heads, tokens, head_dim]."""
+    _check(_native().cache8_read(cache, first, n, step, _struct(k_out), _struct(v_out), stream), "dkv_cache8_read")
+
+
+def dkv_cache8_attend(cache: int, first: int, n: int, step: int, q, out, lse=None, causal=False, stream=None) -> None:
+    """Attention of q [n, n_q_heads, nq, head_dim] over the sequences' rows into out (fp32) and lse (fp32 [n, n_q_heads, nq])."""
+    _check(_native().cache8_attend(cache, first, n, step, _struct(q), _struct(out), lse, causal, stream), "dkv_cache8_attend")
+
+
+def dkv_cache8_fork(cache: int, src: int, dst: int, n: int, step: int, stream=None) -> None:
+    """Sequences dst, dst + step, .. share the pages of src, src + step, .."""
+    _check(_native().cache8_fork(cache, src, dst, n, step, stream), "dkv_cache8_fork")
+
+
+def dkv_cache8_compact(cache: int, first: int, n: int, step: int, idx, count=None, stream=None, heads: int = 0, cols: int = 0) -> None:
+    """Every KV head keeps rows idx[i, h, :count[i]] (int32 [n, n_kv_heads, cols], device); heads, cols: where idx is an address."""
+    _check(_native().cache8_compact(cache, first, n, step, idx, heads, cols, count, stream), "dkv_cache8_compact")
+
+
+def dkv_cache8_trim(cache: int, first: int, n: int, step: int, keep=None, drop: int = 0, stream=None) -> None:
+    """Cut sequences to keep[i] rows (int32 [n], device), or by `drop`; pages behind the last row are given back."""
+    _check(_native().cache8_trim(cache, first, n, step, keep, drop, stream), "dkv_cache8_trim")
+
+
+def dkv_cache8_views(cache: int) -> dict:
+    """Device addresses of a cache's integers: len [n_seqs], held [n_seqs], table [n_seqs, max_pages], refs [n_pages]."""
+    v = [ctypes.c_void_p() for _ in range(4)]
+    _check(load().dkv_cache8_views(cache, *[ctypes.byref(x) for x in v]), "dkv_cache8_views")
+    return dict(zip(("len", "held", "table", "refs"), (x.value for x in v)))
+
+
+def dkv_cache8_status(cache: int):
+    """(code, words) of what the device found since the last report; see include/dkv.h."""
+    buf = (ctypes.c_int32 * 8)()
+    code = load().dkv_cache8_status(cache, buf)
+    return code, list(buf)
+
+
+def dkv_cache8_last_cuda_error(cache: int) -> int:
+    return load().dkv_cache8_last_cuda_error(cache)

@@ -14,7 +14,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdkv.so")
-SOURCES = ["dkv.cu"]
+SOURCES = ["dkv.cu", "cache8.cu"]
 PYCALL = os.path.join(HERE, "_dkv_pycall.so")
 PYCALL_TORCH = PYCALL + ".torch"        # beside it: the torch version it was linked with
 PYCALL_SOURCE = os.path.join(CSRC, "pycall.cpp")
@@ -77,7 +77,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if force or _stale(LIB, kernels + [HEADER]):
         # uncompressed: unpacking the device code takes the first dkv_create of a process 7 ms and more (10 -> 17-30)
         _run([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "--no-compress", "-Xptxas", "-v" if verbose else "-O3",
+              "-shared", "-Xcompiler", "-fPIC", "--no-compress", "--threads", str(len(SOURCES)), "-Xptxas", "-v" if verbose else "-O3",
               "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES], verbose)
     if torch_version() and (force or _stale(PYCALL, [PYCALL_SOURCE, HEADER]) or pycall_built_for() != torch_version()):
         _build_pycall(verbose)

@@ -11,6 +11,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <stdint.h>
+
 #include <exception>
 
 #include "../../include/dkv.h"
@@ -137,12 +139,87 @@ DKV_PY(get_counts, 3, CTX(0) PTR(o, 1) STREAM(2), dkv_get_counts(c, (int32_t*)o,
 DKV_PY(memcpy_to_host, 5, CTX(0) PTR(dst, 1) PTR(src, 2) SIZE(bytes, 3) STREAM(4), dkv_memcpy_to_host(c, dst, src, bytes, st))
 DKV_PY(kept_sorted, 4, CTX(0) INT(l, 1) PTR(o, 2) STREAM(3), dkv_kept_sorted(c, l, (int32_t*)o, st))
 
+// A strided tensor [batch, heads, tokens, head_dim] on a GPU, None (NULL), or the address of a dkv_rows.  A tensor that has not
+// this form becomes one without a type, which the library refuses.
+struct Rows {
+  dkv_rows own;
+  const dkv_rows* p = nullptr;
+  bool take(PyObject* x) {
+    if (x == Py_None) return true;
+    if (!THPVariable_Check(x)) {
+      void* at;
+      if (!address(x, &at)) return false;
+      p = static_cast<const dkv_rows*>(at);
+      return true;
+    }
+    const at::Tensor& t = THPVariable_Unpack(x);
+    own = {};
+    own.type = -1;
+    p = &own;
+    if (!t.is_cuda() || t.dim() != 4 || (t.size(3) > 1 && t.stride(3) != 1)) return true;
+    int32_t size[4];
+    for (int i = 0; i < 4; ++i) {
+      if (t.size(i) > INT32_MAX) return true;
+      size[i] = (int32_t)t.size(i);
+    }
+    switch (t.scalar_type()) {
+      case at::kBFloat16: own.type = DKV_BF16; break;
+      case at::kHalf: own.type = DKV_F16; break;
+      case at::kFloat: own.type = DKV_F32; break;
+      case at::kShort: case at::kUInt16: own.type = DKV_RAW16; break;
+      default: return true;
+    }
+    own.data = t.data_ptr();
+    own.batch = size[0]; own.heads = size[1]; own.tokens = size[2]; own.head_dim = size[3];
+    own.batch_stride = t.stride(0); own.head_stride = t.stride(1); own.token_stride = t.stride(2);
+    return true;
+  }
+};
+// A contiguous tensor of `need` 32-bit numbers at least on a GPU, None (NULL), or an address.  *bad: it is not that.
+bool numbers(PyObject* x, c10::ScalarType type, int64_t need, void** out, bool* bad) {
+  if (!THPVariable_Check(x)) return address(x, out);
+  const at::Tensor& t = THPVariable_Unpack(x);
+  *bad = *bad || !t.is_cuda() || t.scalar_type() != type || !t.is_contiguous() || t.numel() < need;
+  *out = t.data_ptr();
+  return true;
+}
+// Tokens of a batch in a tensor that take() accepted.
+int64_t tokens_of(const Rows& r) { return r.p ? (int64_t)r.p->batch * r.p->tokens : 0; }
+
+#define CACHE(I) void* cp_; if (!address(a[I], &cp_)) return nullptr; dkv_cache8* c = static_cast<dkv_cache8*>(cp_); bool bad = false; (void)bad;
+#define ROWS(V, I) Rows V; if (!V.take(a[I])) return nullptr;
+#define INTS(V, I, NEED) void* V##_p; if (!numbers(a[I], at::kInt, NEED, &V##_p, &bad)) return nullptr; const int32_t* V = static_cast<const int32_t*>(V##_p);
+#define SEQS INT(first, 1) INT(n, 2) INT(step, 3)
+
+DKV_PY(rotate, 8, bool bad = false; PTR(r, 0) ROWS(x, 2) ROWS(xo, 3) ROWS(y, 4) ROWS(yo, 5) INTS(pos, 1, tokens_of(x)) INT(tr, 6) STREAM(7),
+       bad ? DKV_ERR_INVALID_ARG : dkv_rotate((const dkv_rotary*)r, pos, x.p, xo.p, y.p, yo.p, tr, st))
+DKV_PY(cache8_reserve, 7, CACHE(0) SEQS INTS(rows, 4, n) INT(add, 5) STREAM(6),
+       bad ? DKV_ERR_INVALID_ARG : dkv_cache8_reserve(c, first, n, step, rows, add, st))
+DKV_PY(cache8_append, 10, CACHE(0) SEQS ROWS(k, 4) ROWS(v, 5) INTS(rows, 6, n) PTR(r, 7) INTS(pos, 8, n) STREAM(9),
+       bad ? DKV_ERR_INVALID_ARG : dkv_cache8_append(c, first, n, step, k.p, v.p, rows, (const dkv_rotary*)r, pos, st))
+DKV_PY(cache8_read, 7, CACHE(0) SEQS ROWS(k, 4) ROWS(v, 5) STREAM(6), dkv_cache8_read(c, first, n, step, k.p, v.p, st))
+DKV_PY(cache8_attend, 9, CACHE(0) SEQS ROWS(q, 4) ROWS(o, 5)
+       void* lse; if (!numbers(a[6], at::kFloat, q.p ? tokens_of(q) * q.p->heads : 0, &lse, &bad)) return nullptr; INT(causal, 7) STREAM(8),
+       bad ? DKV_ERR_INVALID_ARG : dkv_cache8_attend(c, first, n, step, q.p, o.p, (float*)lse, causal, st))
+DKV_PY(cache8_fork, 6, CACHE(0) INT(from, 1) INT(to, 2) INT(n, 3) INT(step, 4) STREAM(5), dkv_cache8_fork(c, from, to, n, step, st))
+// idx: a tensor [n, heads, cols], or an address with `heads` and `cols`.
+DKV_PY(cache8_compact, 9, CACHE(0) SEQS INTS(idx, 4, 0) INT(heads, 5) INT(cols, 6) INTS(count, 7, n) STREAM(8)
+       if (THPVariable_Check(a[4])) {
+         const at::Tensor& t = THPVariable_Unpack(a[4]);
+         bad = bad || t.dim() != 3 || t.size(0) != n || t.size(1) > INT32_MAX || t.size(2) > INT32_MAX;
+         if (!bad) { heads = (int32_t)t.size(1); cols = (int32_t)t.size(2); }
+       },
+       bad ? DKV_ERR_INVALID_ARG : dkv_cache8_compact(c, first, n, step, idx, heads, cols, count, st))
+DKV_PY(cache8_trim, 7, CACHE(0) SEQS INTS(keep, 4, n) INT(drop, 5) STREAM(6),
+       bad ? DKV_ERR_INVALID_ARG : dkv_cache8_trim(c, first, n, step, keep, drop, st))
+
 #define ENTRY(NAME) {#NAME, (PyCFunction)(void*)py_##NAME, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     ENTRY(reset), ENTRY(score), ENTRY(score_lse), ENTRY(score_static), ENTRY(set_scores), ENTRY(select_topk),
     ENTRY(rebudget), ENTRY(compact), ENTRY(compact_all), ENTRY(run_prefill_pass), ENTRY(run_prefill_pass_lse),
     ENTRY(run_prefill_pass_host), ENTRY(apply_policy), ENTRY(select_positions), ENTRY(decode_attend),
-    ENTRY(get_counts), ENTRY(kept_sorted), ENTRY(memcpy_to_host), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(get_counts), ENTRY(kept_sorted), ENTRY(memcpy_to_host), ENTRY(rotate), ENTRY(cache8_reserve), ENTRY(cache8_append),
+    ENTRY(cache8_read), ENTRY(cache8_attend), ENTRY(cache8_fork), ENTRY(cache8_compact), ENTRY(cache8_trim), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_dkv_pycall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
