@@ -114,7 +114,7 @@ constexpr int kMostQueries = 64;               // query rows of a KV head
 
 template <int D, int QB, int kKind>
 cudaError_t set_attend_smem() {
-  return cudaFuncSetAttribute(attend8_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D, QB>());
+  return cudaFuncSetAttribute(attend8_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
 }
 template <int D>
 cudaError_t set_attend_smem(int kind) {
@@ -152,7 +152,7 @@ cudaError_t with_shape(const dkv_cache8* c, F f) {
 
 template <int D, int QB, int kKind>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
-  return launch_pdl(attend8_kernel<D, QB, kKind>, dim3(c->n_sms), kAttendWarps * 32, (size_t)attend_smem<D, QB>(), 1, st, c->view, a);
+  return launch_pdl(attend8_kernel<D, QB, kKind>, dim3(std::min(c->n_sms, 256)), kAttendWarps * 32, (size_t)attend_smem<D>(), 1, st, c->view, a);
 }
 template <int D>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
@@ -446,6 +446,7 @@ int dkv_cache8_status(dkv_cache8* c, int32_t* host_status) {
   host_status[1] = status[1] == INT_MAX ? -1 : status[1];
   host_status[2] = pages;
   host_status[3] = (int32_t)(c->launches & 0xFFFFFFFF); host_status[4] = (int32_t)(c->launches >> 32);
+  if (status[0] & kTimeout) return DKV_ERR_TIMEOUT;
   if (status[0] & (kNoPages | kTableFull)) return DKV_ERR_NOMEM;
   return status[0] & kNoRoom ? DKV_ERR_STATE : status[0] & kBadArgument ? DKV_ERR_INVALID_ARG : DKV_OK;
 }

@@ -9,8 +9,10 @@
 // Codes lie in the order in which a warp of the attention kernel takes them as operands of m16n8k16, so that its loads are
 // 512 consecutive bytes and need neither shared memory nor a transposition (attend8.cuh):
 //   keys    per 16 rows: [half of 8 rows][panel of 64 dims][row][64 dims];
-//   values  per 16 rows: [32 dims][row pair t = (row % 8) / 2][lane g][word w][row half][row parity], which is dim
-//           32 p + 16 (w / 2) + 4 (g / 2) + 2 (w % 2) + g % 2: one 32-bit word is the operand of one dim and four rows.
+//   values  per 16 rows: [32 dims][row pair t = (row % 8) / 2][place][word w][row half][row parity], place (g + 2 t) % 8 being dim
+//           32 p + 16 (w / 2) + 4 (g / 2) + 2 (w % 2) + g % 2: one 32-bit word is the operand of one dim and four rows, a row lies
+//           in 128 bytes of every 512, and eight lanes that read together find their 16 bytes in different banks.
+// int8 codes are held with 128 added, as bytes that a permutation turns into fp16 numbers.
 #pragma once
 #include <cuda_fp8.h>
 #include "common.cuh"
@@ -20,7 +22,7 @@ namespace dkv {
 
 constexpr int kE4m3 = 0, kInt8 = 1;
 // Status bits a kernel leaves (dkv_cache8_status).
-constexpr int kNoPages = 1, kTableFull = 2, kNoRoom = 4, kBadArgument = 8, kNotFinite = 16;
+constexpr int kNoPages = 1, kTableFull = 2, kNoRoom = 4, kBadArgument = 8, kNotFinite = 16, kTimeout = 32;
 
 // What kernels see of a cache.
 struct Cache8 {
@@ -47,8 +49,8 @@ template <int D>
 __device__ __forceinline__ int key_at(int r, int d) { return (r >> 4) * 16 * D + ((r >> 3) & 1) * 8 * D + (d >> 6) * 512 + (r & 7) * 64 + (d & 63); }
 template <int D>
 __device__ __forceinline__ int value_at(int r, int d) {
-  const int u = d & 15, g = 2 * (u >> 2) + (u & 1), w = 2 * ((d >> 4) & 1) + ((u >> 1) & 1);
-  return (r >> 4) * 16 * D + (d >> 5) * 512 + ((r & 7) >> 1) * 128 + g * 16 + w * 4 + ((r >> 3) & 1) * 2 + (r & 1);
+  const int u = d & 15, t = (r & 7) >> 1, g = 2 * (u >> 2) + (u & 1), w = 2 * ((d >> 4) & 1) + ((u >> 1) & 1);
+  return (r >> 4) * 16 * D + (d >> 5) * 512 + t * 128 + ((g + 2 * t) & 7) * 16 + w * 4 + ((r >> 3) & 1) * 2 + (r & 1);
 }
 
 // Exponent of the smallest power of two s >= 2^-126 with most <= largest code * s; most is finite and not negative.
@@ -66,10 +68,10 @@ __device__ __forceinline__ unsigned int code_pair(float a, float b, int kind) {
   a = a == a ? a : 0.f; b = b == b ? b : 0.f;
   if (kind == kE4m3) return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
   const int x = __float2int_rn(fminf(fmaxf(a, -127.f), 127.f)), y = __float2int_rn(fminf(fmaxf(b, -127.f), 127.f));
-  return (x & 0xFF) | ((y & 0xFF) << 8);
+  return (x + 128) | (y + 128) << 8;
 }
 __device__ __forceinline__ float code_value(unsigned int byte, int kind) {
-  if (kind == kInt8) return (float)(signed char)byte;
+  if (kind == kInt8) return (float)((int)byte - 128);
   return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
 }
 
@@ -243,7 +245,7 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
           }
           reinterpret_cast<uint4*>(code_s)[q] = v;
         }
-      } else if (r1 < R) {                                                   // rows without a value yet are zeros
+      } else if (r1 < R) {                                                   // rows without a value yet
         for (int q = tid; q < R * D / 16; q += kRowThreads) reinterpret_cast<uint4*>(code_s)[q] = make_uint4(0, 0, 0, 0);
       }
       __syncthreads();
