@@ -30,7 +30,7 @@ struct AttendArgs {
   float* out;                // [n][Hq][nq][D], strides below
   long long out_batch, out_head, out_token;
   float* lse;                // [n][Hq][nq] or null
-  float* scratch;            // [2 blocks][rows of a head, in whole QB] partial results, (reference, sum) behind them
+  float* scratch;            // [2 slices][rows of a head, in whole QB] partial results, (reference, sum) behind them
   unsigned int* tickets;     // [n * Hkv], zero between launches
   int first, step, n, nq, rows, G, causal, slots;
   float scale2;              // log2(e) / sqrt(D)
@@ -71,6 +71,11 @@ __device__ __forceinline__ void split_half(float a, float b, uint32_t& hi, uint3
 // Natural logarithm of a query's denominator: sum of weights relative to a reference.
 __device__ __forceinline__ float log_sum(float ref, float sum) {
   return sum == 0.f ? -INFINITY : (ref - kLift + log2f(sum)) * 0.6931471805599453f;
+}
+
+__device__ __forceinline__ float* out_row(const AttendArgs& a, int i, int h, int row) { return a.out + i * a.out_batch + (h * a.G + row / a.nq) * a.out_head + row % a.nq * a.out_token; }
+__device__ __forceinline__ void store_lse(const AttendArgs& a, int Hkv, int i, int h, int row, float ref, float sum) {
+  if (a.lse) a.lse[((size_t)(i * Hkv + h) * a.G + row / a.nq) * a.nq + row % a.nq] = log_sum(ref, sum);
 }
 
 // One warp: QB (8 or 16) query rows against the chunks of 32 rows it takes.  Lane (g, t) = (lane / 4, lane % 4) holds query
@@ -227,19 +232,92 @@ struct AttendWarp {
     }
   }
 
-  // Results as rows in part[QB][D + 4], (reference, sum) in ml[QB].
-  __device__ __forceinline__ void park(float* part, float2* ml, int g, int t) {
+  // Every lane's sums become those of all rows the warp has seen, the two parts of the weights' products one.
+  __device__ __forceinline__ void add_up() {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       sum[h] += __shfl_xor_sync(0xFFFFFFFFu, sum[h], 1);
       sum[h] += __shfl_xor_sync(0xFFFFFFFFu, sum[h], 2);
+    }
+    if constexpr (QB == 8) {
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) { acc[j][0] += acc[j][2]; acc[j][1] += acc[j][3]; }
+    }
+  }
+  // Dims 16 m + 4 t .. + 3 of query row g + 8 h.
+  __device__ __forceinline__ float4 piece(int h, int m) const { return make_float4(acc[2 * m][2 * h], acc[2 * m][2 * h + 1], acc[2 * m + 1][2 * h], acc[2 * m + 1][2 * h + 1]); }
+  // Results as rows in part[QB][D + 4], (reference, sum) in ml[QB].
+  __device__ __forceinline__ void park(float* part, float2* ml, int g, int t) const {
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
       if (t == 0) ml[g + 8 * h] = make_float2(ref[h], sum[h]);
 #pragma unroll
+      for (int m = 0; m < D / 16; ++m) *reinterpret_cast<float4*>(part + (g + 8 * h) * (D + 4) + 16 * m + 4 * t) = piece(h, m);
+    }
+  }
+  // A result as it lies in the registers: [kHalves][D/16][32] pieces, then (reference, sum) of every row.
+  __device__ __forceinline__ void save(float* part, int lane, int g, int t) const {
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      if (t == 0) __stcg(reinterpret_cast<float2*>(part + QB * D) + g + 8 * h, make_float2(ref[h], sum[h]));
+#pragma unroll
+      for (int m = 0; m < D / 16; ++m) __stcg(reinterpret_cast<float4*>(part) + (h * (D / 16) + m) * 32 + lane, piece(h, m));
+    }
+  }
+  // The saved results part(0), part(1), .. added up in that order.
+  template <typename F>
+  __device__ __forceinline__ void merge(F part, int parts, int lane, int g) {
+    constexpr int kFlight = 256 / D;                 // parts whose loads are in flight together, as many as the registers take
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      float m = -INFINITY, l = 0.f;
+      float4 r[D / 16];
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) r[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int p0 = 0; p0 < parts; p0 += 8) {
+        float2 ml[8];
+#pragma unroll
+        for (int f = 0; f < 8; ++f) ml[f] = __ldcg(reinterpret_cast<const float2*>(part(min(p0 + f, parts - 1)) + QB * D) + g + 8 * h);
+#pragma unroll
+        for (int f = 0; f < 8; ++f) m = fmaxf(m, ml[f].x);
+      }
+      for (int p0 = 0; p0 < parts; p0 += kFlight) {
+        float2 ml[kFlight];
+        float4 y[kFlight][D / 16];
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) {
+          const float* from = part(min(p0 + f, parts - 1));
+          ml[f] = __ldcg(reinterpret_cast<const float2*>(from + QB * D) + g + 8 * h);
+#pragma unroll
+          for (int x = 0; x < D / 16; ++x) y[f][x] = __ldcg(reinterpret_cast<const float4*>(from) + (h * (D / 16) + x) * 32 + lane);
+        }
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) {
+          const float k = p0 + f < parts && ml[f].y != 0.f ? fast_exp2(ml[f].x - m) : 0.f;      // (a part may have no row that this query sees)
+          l = p0 + f < parts ? fmaf(ml[f].y, k, l) : l;
+          if (p0 + f < parts) {
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) { r[x].x = fmaf(y[f][x].x, k, r[x].x); r[x].y = fmaf(y[f][x].y, k, r[x].y); r[x].z = fmaf(y[f][x].z, k, r[x].z); r[x].w = fmaf(y[f][x].w, k, r[x].w); }
+          }
+        }
+      }
+      ref[h] = m; sum[h] = l;
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) { acc[2 * x][2 * h] = r[x].x; acc[2 * x][2 * h + 1] = r[x].y; acc[2 * x + 1][2 * h] = r[x].z; acc[2 * x + 1][2 * h + 1] = r[x].w; }
+    }
+  }
+  __device__ __forceinline__ void store(const AttendArgs& a, int Hkv, int i, int h, int g, int t) const {
+#pragma unroll
+    for (int k = 0; k < kHalves; ++k) {
+      const int row = g + 8 * k;
+      if (row >= a.rows) continue;
+      const float inv = sum[k] == 0.f ? 0.f : 1.f / sum[k];
+      float* to = out_row(a, i, h, row);
+      if (t == 0) store_lse(a, Hkv, i, h, row, ref[k], sum[k]);
+#pragma unroll
       for (int m = 0; m < D / 16; ++m) {
-        float4 o;
-        if (QB == 8) o = make_float4(acc[2 * m][0] + acc[2 * m][2], acc[2 * m][1] + acc[2 * m][3], acc[2 * m + 1][0] + acc[2 * m + 1][2], acc[2 * m + 1][1] + acc[2 * m + 1][3]);
-        else o = make_float4(acc[2 * m][2 * h], acc[2 * m][2 * h + 1], acc[2 * m + 1][2 * h], acc[2 * m + 1][2 * h + 1]);
-        *reinterpret_cast<float4*>(part + (g + 8 * h) * (D + 4) + 16 * m + 4 * t) = o;
+        const float4 v = piece(k, m);
+        *reinterpret_cast<float4*>(to + 16 * m + 4 * t) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       }
     }
   }
@@ -269,67 +347,144 @@ __device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity) {
   return false;
 }
 
-// The rows of every (sequence, head) are taken in chunks of 32, kAttendWarps chunks a group, the groups of all heads as one sequence
-// that is cut into one equal slice a block; a head with one group is never cut.  In a slice the warps deal the chunks of a head
-// out among themselves and merge through shared memory; a head that lies in several slices is merged by the block that arrives
+// A warp's ring and the chunks that run through it.
+template <int D>
+struct Ring {
+  static constexpr int kHalfBytes = kAttendRows * D, kChunkBytes = 2 * kHalfBytes, kBytes = kAttendStages * kChunkBytes;
+  unsigned char* at;
+  uint32_t at_s, bar_s;
+  int stage = 0, phase = 0;                            // of the next chunk that is waited for
+  bool broken = false;                                 // a wait ran out: nothing more is asked for or waited for
+
+  __device__ __forceinline__ void start(unsigned char* ring, unsigned long long* bars, int lane) {
+    at = ring;
+    at_s = (uint32_t)__cvta_generic_to_shared(ring); bar_s = (uint32_t)__cvta_generic_to_shared(bars);
+    if (lane == 0) {
+      for (int i = 0; i < kAttendStages; ++i) ring_init(bar_s + i * 8);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+  }
+  // What is still on its way ends before the block does.
+  __device__ __forceinline__ void finish() {
+    if (broken)
+      for (int i = 0; i < kAttendStages; ++i) ring_wait(bar_s + i * 8, i < stage ? phase ^ 1 : phase);
+  }
+  // Adds `count` chunks of head h to w: chunk x is rows first + 32 step x and on.
+  template <int QB, int kKind>
+  __device__ __forceinline__ void run(AttendWarp<D, QB, kKind>& w, const typename AttendWarp<D, QB, kKind>::Raw& raw, const Cache8& c, const AttendArgs& a,
+                                      const int* table, int h, int c0, int len, int first, int step, int count, int lane, int g, int t) {
+    // page and scales of the next 32 chunks, one a lane
+    int page = 0;
+    float2 sc = make_float2(0.f, 0.f);
+    auto look = [&](int x0) {
+      const int x = x0 + lane;
+      if (x < count) {
+        page = table[(first + x * step * kAttendRows) / c.R];
+        sc = *reinterpret_cast<const float2*>(c.scales + region(c, page, h, 0));
+      }
+    };
+    auto fetch = [&](int x, int into) {                // chunk x on its way into its place of the ring
+      if (x >= count || broken) return;
+      const int row = first + x * step * kAttendRows, p = __shfl_sync(0xFFFFFFFFu, page, x & 31);
+      if (lane == 0) {
+        const unsigned char* k = c.pages + region(c, p, h, 0) * (size_t)(c.R * D) + (row % c.R) * D;
+        const uint32_t bar = bar_s + into * 8, to = at_s + into * kChunkBytes;
+        ring_expect(bar, kChunkBytes);
+        if (c.R == kAttendRows) ring_copy(to, k, kChunkBytes, bar);
+        else { ring_copy(to, k, kHalfBytes, bar); ring_copy(to + kHalfBytes, k + c.R * D, kHalfBytes, bar); }
+      }
+    };
+    look(0);
+#pragma unroll
+    for (int x = 0; x < kAttendStages - 1; ++x) fetch(x, (stage + x) % kAttendStages);
+    w.start(raw, a, c0, len, c.io, g);
+    float2 now = sc;                                   // scales of the chunks being worked on (`sc` runs ahead)
+    for (int x = 0; x < count; ++x) {
+      if ((x & 31) == 0) now = sc;
+      if (((x + kAttendStages - 1) & 31) == 0) look(x + kAttendStages - 1);
+      __syncwarp();                                    // every lane is done with the place that is filled next
+      fetch(x + kAttendStages - 1, (stage + kAttendStages - 1) % kAttendStages);
+      if (!broken) broken = !__all_sync(0xFFFFFFFFu, ring_wait(bar_s + stage * 8, phase));
+      const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
+      const unsigned char* k = at + stage * kChunkBytes;
+      if (!broken) w.add(reinterpret_cast<const uint4*>(k), reinterpret_cast<const uint4*>(k + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, first + x * step * kAttendRows, lane, t);
+      if (++stage == kAttendStages) { stage = 0; phase ^= 1; }
+    }
+  }
+};
+
+// Lengths of a launch's sequences into len_s, and before each, and in all, the sum of units_of(length) * Hkv into prefix_s.
+template <typename F>
+__device__ __forceinline__ void sum_units(const Cache8& c, const AttendArgs& a, int* len_s, int* prefix_s, int* scan_s, F units_of) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (a.n + kAttendWarps * 32 - 1) / (kAttendWarps * 32), i0 = min(a.n, tid * per), i1 = min(a.n, i0 + per);
+  int mine = 0;
+  for (int i = i0; i < i1; ++i) { len_s[i] = c.len[a.first + i * a.step]; mine += units_of(len_s[i]) * c.Hkv; }
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xFFFFFFFFu, inc, o); if (lane >= o) inc += y; }
+  if (lane == 31) scan_s[warp] = inc;
+  __syncthreads();
+  int at = inc - mine;
+  for (int w = 0; w < warp; ++w) at += scan_s[w];
+  for (int i = i0; i < i1; ++i) { prefix_s[i] = at; at += units_of(len_s[i]) * c.Hkv; }
+  if (i0 < i1 && i1 == a.n) prefix_s[a.n] = at;
+  __syncthreads();
+}
+__device__ __forceinline__ int chunks_of(int len) { return (len + kAttendRows - 1) / kAttendRows; }
+
+// A sequence of units cut into equal slices.
+struct Slices {
+  int total, count;
+  __device__ __forceinline__ int begin(int x) const { return (int)((long long)total * x / count); }
+  __device__ __forceinline__ int owner(int u) const { return (int)(((long long)(u + 1) * count + total - 1) / total) - 1; }       // the slice that holds unit u
+};
+// The (sequence, head) that unit u belongs to: its place in the call, head, first unit and units.
+struct HeadAt { int i, h, u0, units; };
+__device__ __forceinline__ HeadAt head_at(int u, const int* prefix_s, int n, int Hkv) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (prefix_s[mid] <= u) lo = mid; else hi = mid - 1; }
+  const int units = (prefix_s[lo + 1] - prefix_s[lo]) / Hkv, h = (u - prefix_s[lo]) / units;
+  return {lo, h, prefix_s[lo] + h * units, units};
+}
+// Few heads.  The rows of every (sequence, head) are taken in chunks of 32, kAttendWarps chunks a group, the groups of all heads as one
+// sequence that is cut into one equal slice a block; a head with one group is never cut.  In a slice the warps deal the chunks of a
+// head out among themselves and merge through shared memory; a head that lies in several slices is merged by the block that arrives
 // last (a ticket a head), in slice order, so that nothing depends on which that is.
 template <int D, int QB, int kKind>
 __global__ void __launch_bounds__(kAttendWarps * 32, 1)
 attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendArgs a) {
   using Warp = AttendWarp<D, QB, kKind>;
-  constexpr int NW = kAttendWarps, ST = kAttendStages, kHalfBytes = kAttendRows * D, kChunkBytes = 2 * kHalfBytes;
+  constexpr int NW = kAttendWarps;
   static_assert(NW * QB * (D + 4) * 4 + NW * QB * 8 <= attend_smem<D>() && 256 * QB * 12 <= attend_smem<D>());   // merges, of at most 256 parts
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ int prefix_s[kAttendMaxSeqs + 1], len_s[kAttendMaxSeqs];
   __shared__ int scan_s[NW];
   __shared__ unsigned int ticket_s;
-  __shared__ __align__(8) unsigned long long bar_s[NW * ST];
+  __shared__ __align__(8) unsigned long long bar_s[NW * kAttendStages];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  unsigned char* ring = smem + (size_t)warp * ST * kChunkBytes;
-  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring), bar_at = (uint32_t)__cvta_generic_to_shared(bar_s + warp * ST);
+  Ring<D> ring;
   float* part_s = reinterpret_cast<float*>(smem);
   float2* ml_s = reinterpret_cast<float2*>(part_s + NW * QB * (D + 4));
   pdl_launch();
-  if (lane == 0) {
-    for (int i = 0; i < ST; ++i) ring_init(bar_at + i * 8);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  __syncwarp();
+  ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane);
   pdl_wait();
-  auto chunks_of = [&](int len) { return (len + kAttendRows - 1) / kAttendRows; };
-  auto groups_of = [&](int len) { return max(1, (chunks_of(len) + NW - 1) / NW) * c.Hkv; };
-  {
-    const int per = (a.n + NW * 32 - 1) / (NW * 32), i0 = min(a.n, tid * per), i1 = min(a.n, i0 + per);
-    int mine = 0;
-    for (int i = i0; i < i1; ++i) { len_s[i] = c.len[a.first + i * a.step]; mine += groups_of(len_s[i]); }
-    int inc = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xFFFFFFFFu, inc, o); if (lane >= o) inc += y; }
-    if (lane == 31) scan_s[warp] = inc;
-    __syncthreads();
-    int at = inc - mine;
-    for (int w = 0; w < warp; ++w) at += scan_s[w];
-    for (int i = i0; i < i1; ++i) { prefix_s[i] = at; at += groups_of(len_s[i]); }
-    if (i0 < i1 && i1 == a.n) prefix_s[a.n] = at;
-    __syncthreads();
-  }
-  const int total = prefix_s[a.n], slices = min((int)gridDim.x, total), own = blockIdx.x;
-  if (own >= slices) return;
-  auto slice = [&](int x) { return (int)((long long)total * x / slices); };
-  auto owner = [&](int u) { return (int)(((long long)(u + 1) * slices + total - 1) / total) - 1; };     // the slice that holds group u
-  const int u1 = slice(own + 1), passes = (a.rows + QB - 1) / QB;
-  int stage = 0, phase = 0;                            // of the next chunk this warp waits for
-  bool broken = false;                                 // a wait ran out: nothing more is asked for or waited for
-  for (int u = slice(own); u < u1;) {
-    int lo = 0, hi = a.n - 1;
-    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (prefix_s[mid] <= u) lo = mid; else hi = mid - 1; }
-    const int groups = (prefix_s[lo + 1] - prefix_s[lo]) / c.Hkv, h = (u - prefix_s[lo]) / groups, u0 = prefix_s[lo] + h * groups;
-    const int seq = a.first + lo * a.step, len = len_s[lo], end = min(u1, u0 + groups);
-    const int ch0 = (u - u0) * NW, ch1 = min(chunks_of(len), (end - u0) * NW);
-    const bool begins = u == u0, whole = begins && end == u0 + groups;
+  sum_units(c, a, len_s, prefix_s, scan_s, [](int len) { return max(1, (chunks_of(len) + NW - 1) / NW); });
+  // as many slices a head as there can be, and no slice in two heads, where that leaves few blocks without one
+  const int total = prefix_s[a.n], heads = a.n * c.Hkv, even = gridDim.x - gridDim.x % heads;
+  const Slices slices = {total, min(heads <= (int)gridDim.x && even * 8 >= (int)gridDim.x * 7 ? even : (int)gridDim.x, total)};
+  const int own = blockIdx.x;
+  if (own >= slices.count) return;
+  const int u1 = slices.begin(own + 1), passes = (a.rows + QB - 1) / QB;
+  for (int u = slices.begin(own); u < u1;) {
+    const HeadAt at = head_at(u, prefix_s, a.n, c.Hkv);
+    const int lo = at.i, h = at.h, seq = a.first + lo * a.step, len = len_s[lo], end = min(u1, at.u0 + at.units);
+    const int ch0 = (u - at.u0) * NW, ch1 = min(chunks_of(len), (end - at.u0) * NW);
+    const bool begins = u == at.u0, whole = begins && end == at.u0 + at.units;
     const int* table = c.table + (size_t)seq * c.max_pages;
     u = end;
-    const int c_lo = owner(u0), c_hi = owner(u0 + groups - 1);
+    const int c_lo = slices.owner(at.u0), c_hi = slices.owner(at.u0 + at.units - 1);
     // parts: slot 0 of a slice continues a head, slot 1 begins one that others continue
     auto part = [&](int sl, bool first, int pass) { return a.scratch + ((size_t)(2 * sl + first) * a.slots + pass) * (QB * (D + 2)); };
     for (int pass = 0; pass < passes; ++pass) {
@@ -337,57 +492,21 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
       typename Warp::Raw raw;
       const int c0 = pass * QB, mine = max(0, (ch1 - ch0 - warp + NW - 1) / NW);      // this warp's chunks: ch0 + warp + NW x
       Warp::ask(raw, a, lo, h, c0, g, t);
-      // page and scales of the next 32 chunks, one a lane
-      int page = 0;
-      float2 sc = make_float2(0.f, 0.f);
-      auto look = [&](int x0) {
-        const int x = x0 + lane;
-        if (x < mine) {
-          page = table[(ch0 + warp + NW * x) * kAttendRows / c.R];
-          sc = *reinterpret_cast<const float2*>(c.scales + region(c, page, h, 0));
-        }
-      };
-      auto fetch = [&](int x, int into) {              // chunk x on its way into its place of the ring
-        if (x >= mine || broken) return;
-        const int row = (ch0 + warp + NW * x) * kAttendRows;
-        const int p = __shfl_sync(0xFFFFFFFFu, page, x & 31);
-        if (lane == 0) {
-          const unsigned char* k = c.pages + region(c, p, h, 0) * (size_t)(c.R * D) + (row % c.R) * D;
-          const uint32_t bar = bar_at + into * 8, to = ring_at + into * kChunkBytes;
-          ring_expect(bar, kChunkBytes);
-          if (c.R == kAttendRows) ring_copy(to, k, kChunkBytes, bar);
-          else { ring_copy(to, k, kHalfBytes, bar); ring_copy(to + kHalfBytes, k + c.R * D, kHalfBytes, bar); }
-        }
-      };
-      look(0);
-#pragma unroll
-      for (int x = 0; x < ST - 1; ++x) fetch(x, (stage + x) % ST);
-      w.start(raw, a, c0, len, c.io, g);
-      float2 now = sc;                                 // scales of the chunks being worked on (`sc` runs ahead)
-      for (int x = 0; x < mine; ++x) {
-        if ((x & 31) == 0) now = sc;
-        if (((x + ST - 1) & 31) == 0) look(x + ST - 1);
-        __syncwarp();                                  // every lane is done with the place that is filled next
-        fetch(x + ST - 1, (stage + ST - 1) % ST);
-        if (!broken) broken = !__all_sync(0xFFFFFFFFu, ring_wait(bar_at + stage * 8, phase));
-        const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
-        const unsigned char* at = ring + stage * kChunkBytes;
-        if (!broken) w.add(reinterpret_cast<const uint4*>(at), reinterpret_cast<const uint4*>(at + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, (ch0 + warp + NW * x) * kAttendRows, lane, t);
-        if (++stage == ST) { stage = 0; phase ^= 1; }
-      }
-      if (broken && lane == 0) report(c, kTimeout, seq);
+      ring.run(w, raw, c, a, table, h, c0, len, (ch0 + warp) * kAttendRows, NW, mine, lane, g, t);
+      if (ring.broken && lane == 0) report(c, kTimeout, seq);
       __syncthreads();
+      w.add_up();
       w.park(part_s + warp * QB * (D + 4), ml_s + warp * QB, g, t);
       __syncthreads();
       const int pieces = min(QB, a.rows - c0) * (D / 4);
       for (int x = tid; x < pieces; x += NW * 32) {
         float4 v;
         const float2 ml = merge_warps<D, QB, NW>(part_s, ml_s, x, v);
-        const int qi = x / (D / 4), d = x % (D / 4) * 4, row = c0 + qi, hq = h * a.G + row / a.nq, token = row % a.nq;
+        const int qi = x / (D / 4), d = x % (D / 4) * 4;
         if (whole) {
           const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
-          *reinterpret_cast<float4*>(a.out + lo * a.out_batch + hq * a.out_head + token * a.out_token + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-          if (a.lse && d == 0) a.lse[((size_t)lo * c.Hkv * a.G + hq) * a.nq + token] = log_sum(ml.x, ml.y);
+          *reinterpret_cast<float4*>(out_row(a, lo, h, c0 + qi) + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+          if (d == 0) store_lse(a, c.Hkv, lo, h, c0 + qi, ml.x, ml.y);
         } else {
           float* to = part(own, begins, pass);
           __stcg(reinterpret_cast<float4*>(to) + x, v);
@@ -426,12 +545,11 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
         for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
         const float inv = l == 0.f ? 0.f : 1.f / l;
         for (int p = lane; p < parts; p += 32) weight_s[p * QB + qi] = weight(all_s[p * QB + qi]) * inv;
-        const int row = c0 + qi;
-        if (a.lse && lane == 0) a.lse[((size_t)lo * c.Hkv * a.G + h * a.G + row / a.nq) * a.nq + row % a.nq] = log_sum(m, l);
+        if (lane == 0) store_lse(a, c.Hkv, lo, h, c0 + qi, m, l);
       }
       __syncthreads();
       for (int x = tid; x < rows * (D / 4); x += NW * 32) {
-        const int qi = x / (D / 4), row = c0 + qi, hq = h * a.G + row / a.nq, token = row % a.nq;
+        const int qi = x / (D / 4);
         float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int kFlight = 10;                    // parts whose loads are in flight together
         for (int p0 = 0; p0 < parts; p0 += kFlight) {
@@ -448,7 +566,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
               r.x = fmaf(y[f].x, k, r.x); r.y = fmaf(y[f].y, k, r.y); r.z = fmaf(y[f].z, k, r.z); r.w = fmaf(y[f].w, k, r.w);
             }
         }
-        *reinterpret_cast<float4*>(a.out + lo * a.out_batch + hq * a.out_head + token * a.out_token + x % (D / 4) * 4) = r;
+        *reinterpret_cast<float4*>(out_row(a, lo, h, c0 + qi) + x % (D / 4) * 4) = r;
       }
       __syncthreads();
     }
@@ -456,8 +574,65 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
   }
-  if (broken)                                          // what is still on its way ends before the block does
-    for (int i = 0; i < ST; ++i) ring_wait(bar_at + i * 8, i < stage ? phase ^ 1 : phase);
+  ring.finish();
+}
+
+// Many heads.  The chunks of all heads form one sequence that is cut into one equal slice a WARP, so that no warp waits for another:
+// no barrier, and the set-up of one warp's head runs beside the other warps' work.  A head counts kAttendHeadCost chunks more
+// than it has.  A head that lies in one slice is finished there; of the others every warp leaves its part in scratch, as it
+// lies in its registers, and the warp that arrives last for a head (a ticket) merges the parts in slice order.
+constexpr int kAttendHeadCost = 1;
+template <int D, int QB, int kKind>
+__global__ void __launch_bounds__(kAttendWarps * 32, 1)
+attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendArgs a) {
+  using Warp = AttendWarp<D, QB, kKind>;
+  constexpr int NW = kAttendWarps;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ int prefix_s[kAttendMaxSeqs + 1], len_s[kAttendMaxSeqs];
+  __shared__ int scan_s[NW];
+  __shared__ __align__(8) unsigned long long bar_s[NW * kAttendStages];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  Ring<D> ring;
+  pdl_launch();
+  ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane);
+  pdl_wait();
+  sum_units(c, a, len_s, prefix_s, scan_s, [](int len) { return chunks_of(len) + kAttendHeadCost; });
+  // no more slices than units: an empty slice would leave no part, and whoever merges a head counts on one from each
+  const int total = prefix_s[a.n], own = blockIdx.x * NW + warp;
+  const Slices slices = {total, min((int)gridDim.x * NW, total)};
+  if (own >= slices.count) return;
+  const int u1 = slices.begin(own + 1);
+  for (int u = slices.begin(own); u < u1;) {
+    const HeadAt at = head_at(u, prefix_s, a.n, c.Hkv);
+    // units of a head: its cost, then its chunks; a slice that has the cost only leaves the head to the next ones
+    const int seq = a.first + at.i * a.step, len = len_s[at.i], all = at.units - kAttendHeadCost, row0 = at.u0 + kAttendHeadCost;
+    const int end = min(u1, at.u0 + at.units), first = max(0, u - row0), after = max(0, end - row0);
+    u = end;
+    if (after == 0 && all > 0) continue;
+    const bool whole = first == 0 && after == all;
+    const int c_lo = slices.owner(all > 0 ? row0 : at.u0), c_hi = slices.owner(at.u0 + at.units - 1);
+    if (all == 0 && own != c_hi) continue;             // (a head without rows whose cost is several units)
+    Warp w;
+    typename Warp::Raw raw;
+    Warp::ask(raw, a, at.i, at.h, 0, g, t);
+    ring.run(w, raw, c, a, c.table + (size_t)seq * c.max_pages, at.h, 0, len, first * kAttendRows, 1, after - first, lane, g, t);
+    if (ring.broken && lane == 0) report(c, kTimeout, seq);
+    w.add_up();
+    if (whole) { w.store(a, c.Hkv, at.i, at.h, g, t); continue; }
+    auto part = [&](int sl, bool first) { return a.scratch + (size_t)(2 * sl + first) * (QB * (D + 2)); };
+    w.save(part(own, first == 0), lane, g, t);
+    unsigned int* ticket = a.tickets + (size_t)at.i * c.Hkv + at.h;
+    __threadfence();
+    __syncwarp();
+    unsigned int arrived = 0;
+    if (lane == 0) arrived = atomicAdd(ticket, 1u);
+    if (__shfl_sync(0xFFFFFFFFu, arrived, 0) != (unsigned int)(c_hi - c_lo)) continue;
+    __threadfence();
+    w.merge([&](int p) { return part(c_lo + p, p == 0); }, c_hi - c_lo + 1, lane, g);
+    w.store(a, c.Hkv, at.i, at.h, g, t);
+    if (lane == 0) *ticket = 0;
+  }
+  ring.finish();
 }
 
 }  // namespace dkv

@@ -112,9 +112,19 @@ int free_cache(dkv_cache8* c) {
 
 constexpr int kMostQueries = 64;               // query rows of a KV head
 
+int attend_blocks(const dkv_cache8* c) { return std::min(c->n_sms, 256); }
+// A slice a warp where there are so many heads that one does not lie in more than some sixteen slices (a single warp merges them)
+// and the query rows fit one pass; else a slice a block.
+bool attend_by_warps(const dkv_cache8* c, int n, int rows) { return rows <= 16 && (long long)n * c->cfg.n_kv_heads * 16 >= attend_blocks(c) * kAttendWarps; }
+// Floats of scratch: two parts a slice, of 16 rows a warp or of all a block.
+size_t attend_scratch(const dkv_cache8* c) {
+  return (size_t)attend_blocks(c) * 2 * std::max(kAttendWarps * 16, kMostQueries) * (c->cfg.head_dim + 2);
+}
+
 template <int D, int QB, int kKind>
 cudaError_t set_attend_smem() {
-  return cudaFuncSetAttribute(attend8_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
+  const cudaError_t e = cudaFuncSetAttribute(attend8_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(attend8_warps_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
 }
 template <int D>
 cudaError_t set_attend_smem(int kind) {
@@ -152,7 +162,8 @@ cudaError_t with_shape(const dkv_cache8* c, F f) {
 
 template <int D, int QB, int kKind>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
-  return launch_pdl(attend8_kernel<D, QB, kKind>, dim3(std::min(c->n_sms, 256)), kAttendWarps * 32, (size_t)attend_smem<D>(), 1, st, c->view, a);
+  const bool warps = attend_by_warps(c, a.n, a.rows);
+  return launch_pdl(warps ? attend8_warps_kernel<D, QB, kKind> : attend8_kernel<D, QB, kKind>, dim3(attend_blocks(c)), kAttendWarps * 32, (size_t)attend_smem<D>(), 1, st, c->view, a);
 }
 template <int D>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
@@ -273,7 +284,7 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   TRY(cudaMalloc(&c->d_new_table, entries * sizeof(int)));
   TRY(cudaMalloc(&c->d_new_held, sizeof(int) * cfg->n_seqs));
   TRY(cudaMalloc(&c->d_tickets, sizeof(int) * (size_t)cfg->n_seqs * cfg->n_kv_heads));
-  TRY(cudaMalloc(&c->d_scratch, sizeof(float) * 2 * c->n_sms * kMostQueries * (cfg->head_dim + 2)));
+  TRY(cudaMalloc(&c->d_scratch, sizeof(float) * attend_scratch(c)));
   // every code is a number from the start: what rows not yet written hold is multiplied by a weight of zero
   TRY(cudaMemset(v.pages, 0, regions * cfg->page_rows * cfg->head_dim));
   TRY(cudaMemset(v.scales, 0, regions * sizeof(float)));
@@ -371,9 +382,9 @@ int dkv_cache8_attend(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   a.step = step; a.nq = q->tokens; a.rows = G * q->tokens; a.G = G; a.causal = causal != 0;
   a.slots = (a.rows + (a.rows <= 8 ? 7 : 15)) / (a.rows <= 8 ? 8 : 16);
   a.scale2 = kLog2e / sqrtf((float)c->cfg.head_dim);
-  // sequences a launch: their prefix sums fit shared memory, and their groups 31 bits
-  const long long groups = (long long)c->cfg.n_kv_heads * (((long long)c->cfg.max_pages * c->cfg.page_rows) / (kAttendRows * kAttendWarps) + 1);
-  const int most = (int)std::max(1ll, std::min<long long>(kAttendMaxSeqs, INT_MAX / groups));
+  // sequences a launch: their prefix sums fit shared memory, and their units (chunks, at most) 31 bits
+  const long long units = (long long)c->cfg.n_kv_heads * (((long long)c->cfg.max_pages * c->cfg.page_rows) / kAttendRows + kAttendHeadCost);
+  const int most = (int)std::max(1ll, std::min<long long>(kAttendMaxSeqs, INT_MAX / units));
   for (int i = 0; i < n; i += most) {
     a.n = std::min(most, n - i); a.first = first + i * step;
     a.q = static_cast<const char*>(q->data) + (size_t)i * a.q_batch * 2;
