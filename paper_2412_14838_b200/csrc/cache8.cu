@@ -110,6 +110,7 @@ int free_cache(dkv_cache8* c) {
   return DKV_OK;
 }
 
+constexpr int kFewRows = 8;                    // rows a call and sequence up to which a block takes a whole sequence (append8_few_kernel)
 constexpr int kMostQueries = 64;               // query rows of a KV head
 
 int attend_blocks(const dkv_cache8* c) { return std::min(c->n_sms, 256); }
@@ -349,7 +350,9 @@ int dkv_cache8_append(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   }
   const int R = c->cfg.page_rows, pages = (int)std::min<long long>(((long long)k->tokens + R - 2) / R + 1, c->cfg.max_pages);
   C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
-    return launch_pdl(append8_kernel<decltype(d)::value, decltype(r)::value>, dim3(pages, 2 * c->cfg.n_kv_heads, n), kRowThreads, 0, 1, as_stream(stream), c->view, a);
+    constexpr int D = decltype(d)::value, rows = decltype(r)::value;
+    if (k->tokens <= kFewRows) return launch_pdl(append8_few_kernel<D, rows>, dim3(n), std::min(2 * c->cfg.n_kv_heads, kFewWarps) * 32, 0, 1, as_stream(stream), c->view, a);
+    return launch_pdl(append8_kernel<D, rows>, dim3(pages, 2 * c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, as_stream(stream), c->view, a);
   }));
   return DKV_OK;
 }
@@ -361,7 +364,8 @@ int dkv_cache8_read(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const
   const ReadArgs a = {rows8(k_out), rows8(v_out), first, step, k_out->tokens};
   const int R = c->cfg.page_rows, pages = std::min((int)(((long long)k_out->tokens + R - 1) / R), c->cfg.max_pages);
   C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
-    return launch_pdl(read8_kernel<decltype(d)::value, decltype(r)::value>, dim3(pages, 2 * c->cfg.n_kv_heads, n), kRowThreads, 0, 1, as_stream(stream), c->view, a);
+    constexpr int D = decltype(d)::value, rows = decltype(r)::value;
+    return launch_pdl(read8_kernel<D, rows>, dim3(pages, 2 * c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, as_stream(stream), c->view, a);
   }));
   return DKV_OK;
 }
@@ -417,7 +421,8 @@ int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   const int R = c->cfg.page_rows, pages = std::min((int)(((long long)cols + R - 1) / R), c->cfg.max_pages);
   if (pages)
     C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
-      return launch_pdl(compact8_kernel<decltype(d)::value, decltype(r)::value>, dim3(pages, 2 * c->cfg.n_kv_heads, n), kRowThreads, 0, 1, st, c->view, a);
+      constexpr int D = decltype(d)::value, rows = decltype(r)::value;
+      return launch_pdl(compact8_kernel<D, rows>, dim3(pages, 2 * c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, st, c->view, a);
     }));
   C8_LAUNCH(c, launch_pdl(install8_kernel, dim3(n), kSeqThreads, 0, 1, st, c->view, a));
   return DKV_OK;

@@ -44,15 +44,9 @@ __device__ __forceinline__ void report(const Cache8& c, int bit, int seq) {
 }
 __device__ __forceinline__ size_t region(const Cache8& c, int page, int h, int which) { return ((size_t)page * c.Hkv + h) * 2 + which; }
 
-// Place of a code within its region: row r, dim d.
+// Place of a key's code within its region: row r, dim d.
 template <int D>
 __device__ __forceinline__ int key_at(int r, int d) { return (r >> 4) * 16 * D + ((r >> 3) & 1) * 8 * D + (d >> 6) * 512 + (r & 7) * 64 + (d & 63); }
-template <int D>
-__device__ __forceinline__ int value_at(int r, int d) {
-  const int u = d & 15, t = (r & 7) >> 1, g = 2 * (u >> 2) + (u & 1), w = 2 * ((d >> 4) & 1) + ((u >> 1) & 1);
-  return (r >> 4) * 16 * D + (d >> 5) * 512 + t * 128 + ((g + 2 * t) & 7) * 16 + w * 4 + ((r >> 3) & 1) * 2 + (r & 1);
-}
-
 // Exponent of the smallest power of two s >= 2^-126 with most <= largest code * s; most is finite and not negative.
 // 448 = 0x1.Cp8, 127 = 0x1.FCp6.
 __device__ __forceinline__ int scale_exponent(float most, int kind) {
@@ -105,31 +99,67 @@ __device__ __forceinline__ float block_max(float v, float* warp_s) {
   return v;
 }
 
-// Codes of eight dims d..d+7 of row r into a region.
+// What a thread takes of a page: rows 16 blk + 2 t, + 1, + 8, + 9 and dims d..d+7, the four rows that share the words of values.
+struct Quad { Eight row[4]; };
+__device__ __forceinline__ int quad_row(int blk, int t, int k) { return blk * 16 + 2 * t + (k & 1) + 8 * (k >> 1); }
 template <int D>
-__device__ __forceinline__ void put8(unsigned char* to, int r, int d, const Eight& e, float inv, int which, int kind) {
-  unsigned int c[4];
+__device__ __forceinline__ int quad_values_at(int blk, int t, int d, int pair) {       // 8 bytes: dims d + {0, 2}, {1, 3}, {4, 6}, {5, 7}
+  const int g = 2 * ((d & 15) >> 2) + pair;
+  return blk * 16 * D + (d >> 5) * 512 + t * 128 + ((g + 2 * t) & 7) * 16 + ((d >> 4) & 1) * 8;
+}
+// Codes of a quad into a region: keys of rows [from, to), values of all four rows.
+template <int D>
+__device__ __forceinline__ void put_quad(unsigned char* at, int blk, int t, int d, const Quad& q, float inv, int which, int kind, int from, int to) {
+  unsigned int c[4][4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = code_pair(e.x[2 * i] * inv, e.x[2 * i + 1] * inv, kind);
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[k][i] = code_pair(q.row[k].x[2 * i] * inv, q.row[k].x[2 * i + 1] * inv, kind);
   if (which == 0) {
-    *reinterpret_cast<uint2*>(to + key_at<D>(r, d)) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-  } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) to[value_at<D>(r, d + i)] = (unsigned char)(c[i >> 1] >> (i & 1) * 8);
+    for (int k = 0; k < 4; ++k) {
+      const int r = quad_row(blk, t, k);
+      if (r >= from && r < to) *reinterpret_cast<uint2*>(at + key_at<D>(r, d)) = make_uint2(c[k][0] | c[k][1] << 16, c[k][2] | c[k][3] << 16);
+    }
+  } else {
+    unsigned int w[8];                                   // a dim each
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned int x = c[0][i] | c[1][i] << 16, y = c[2][i] | c[3][i] << 16;
+      w[2 * i] = __byte_perm(x, y, 0x6420); w[2 * i + 1] = __byte_perm(x, y, 0x7531);
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int i = 4 * (p >> 1) + (p & 1);
+      *reinterpret_cast<uint2*>(at + quad_values_at<D>(blk, t, d, p)) = make_uint2(w[i], w[i + 2]);
+    }
   }
 }
-template <int D>
-__device__ __forceinline__ Eight get8(const unsigned char* from, int r, int d, float scale, int which, int kind) {
+__device__ __forceinline__ Eight eight_of(unsigned int lo, unsigned int hi, float scale, int kind) {
   Eight e;
-  if (which == 0) {
-    const uint2 v = *reinterpret_cast<const uint2*>(from + key_at<D>(r, d));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e.x[i] = code_value(((i < 4 ? v.x : v.y) >> (i & 3) * 8) & 0xFF, kind) * scale;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) e.x[i] = code_value(from[value_at<D>(r, d + i)], kind) * scale;
-  }
+  for (int i = 0; i < 8; ++i) e.x[i] = code_value(((i < 4 ? lo : hi) >> (i & 3) * 8) & 0xFF, kind) * scale;
   return e;
+}
+// A quad's raw words: keys of rows below `to`, values of all rows.
+struct QuadWords { uint2 v[4]; };
+template <int D>
+__device__ __forceinline__ QuadWords get_words(const unsigned char* at, int blk, int t, int d, int which, int to) {
+  QuadWords q;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = quad_row(blk, t, k);
+    if (which) q.v[k] = *reinterpret_cast<const uint2*>(at + quad_values_at<D>(blk, t, d, k));
+    else q.v[k] = r < to ? *reinterpret_cast<const uint2*>(at + key_at<D>(r, d)) : make_uint2(0, 0);
+  }
+  return q;
+}
+// Row k of a quad as numbers.
+__device__ __forceinline__ Eight row_of(const QuadWords& q, int k, float scale, int which, int kind) {
+  if (which == 0) return eight_of(q.v[k].x, q.v[k].y, scale, kind);
+  // word of dim i: pair 2 (i / 4) + i % 2, half (i / 2) % 2
+  auto byte = [&](int i) { const uint2 v = q.v[2 * (i >> 2) + (i & 1)]; return ((i >> 1 & 1 ? v.y : v.x) >> k * 8) & 0xFF; };
+  return eight_of(byte(0) | byte(1) << 8 | byte(2) << 16 | byte(3) << 24, byte(4) | byte(5) << 8 | byte(6) << 16 | byte(7) << 24, scale, kind);
 }
 
 // ---- rows in ------------------------------------------------------------------------------------------------------------
@@ -147,117 +177,102 @@ struct AppendArgs {
   double turns[128];
 };
 
-// The new rows of one page, head and tensor: their largest magnitude gives the scale, and where the page held rows before, the
-// old scale is a lower bound for it; if it grows, the old codes are rounded again.  Bound by HBM (2 bytes in, 1 out) where rows
-// are many and by latency where there is one.  A page is put together in shared memory and written as a whole, but for a few
-// rows that join a page whose scale stays.  grid (pages a sequence can touch, 2 Hkv, n); the last block of a sequence to arrive
-// (a ticket) makes the rows part of it.
-constexpr int kRowThreads = 256;
+// Eight dims of a new row; keys are turned where the call says so.
+__device__ __forceinline__ Eight new_row(const AppendArgs& a, const unsigned short* line, int d, int pos, bool turn, int io) {
+  Eight x = unpack8(*reinterpret_cast<const uint4*>(line + d), io);
+  if (turn && d < a.rot) {
+    const int half = a.rot / 2;
+    if (a.pairs) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2)
+        if (d + e < a.rot) {
+          float cs, sn;
+          turn_of(pos, a.turns[(d + e) / 2], cs, sn);
+          const float u = x.x[e], w = x.x[e + 1];
+          x.x[e] = a.amplitude * (u * cs - w * sn); x.x[e + 1] = a.amplitude * (u * sn + w * cs);
+        }
+    } else {
+      Eight y;
+      if (a.vec) y = unpack8(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)), io);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (d + e < a.rot) {
+          const bool lower = d + e < half;
+          if (!a.vec) y.x[e] = load16(line[lower ? d + e + half : d + e - half], io);
+          float cs, sn;
+          turn_of(pos, a.turns[lower ? d + e : d + e - half], cs, sn);
+          x.x[e] = a.amplitude * (lower ? x.x[e] * cs - y.x[e] * sn : y.x[e] * sn + x.x[e] * cs);
+        }
+    }
+  }
+  return x;
+}
+__device__ __forceinline__ void largest(const Eight& x, float& most, bool& odd) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float m = fabsf(x.x[e]);
+    if (m < INFINITY) most = fmaxf(most, m); else odd = true;
+  }
+}
+// Whether `add` rows go behind the `len` rows of a sequence; if not, why (a status bit), else 0.
+__device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, const int* table, int len, int held, int add) {
+  if (add < 0 || add > a.cap) return kBadArgument;
+  if ((long long)len + add > (long long)held * c.R) return kNoRoom;
+  return add > 0 && len % c.R && c.refs[table[len / c.R]] != 1 ? kNoRoom : 0;
+}
+
+// Many rows: the new rows of one page, head and tensor.  Their largest magnitude gives the scale; where the page held rows before,
+// the old scale is a lower bound for it and the old codes are rounded again.  A thread has one quad, from 16-bit numbers in
+// registers straight to codes.  Bound by HBM (2 bytes in, 1 out).  grid (pages a sequence can touch, 2 Hkv, n); the last block
+// of a sequence to arrive (a ticket) makes the rows part of it.
 template <int D, int R>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(R * D / 32)
 append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
-  constexpr int kPieces = R * D / 8, kPer = (kPieces + kRowThreads - 1) / kRowThreads;
-  __shared__ __align__(16) unsigned char code_s[R * D];
-  __shared__ float warp_s[kRowThreads / 32];
+  __shared__ float warp_s[R * D / 1024];
   const int tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
   pdl_launch();
   pdl_wait();
   const int len = c.len[seq], held = c.held[seq], add = a.rows ? a.rows[i] : a.cap;
   const int* table = c.table + (size_t)seq * c.max_pages;
-  const bool bad = add < 0 || add > a.cap;
-  bool room = !bad && (long long)len + add <= (long long)held * R;
-  if (room && add > 0 && len % R) room = c.refs[table[len / R]] == 1;
-  if (!room || add == 0) {
-    if (!room && tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) report(c, bad ? kBadArgument : kNoRoom, seq);
+  const int not_ok = no_room(c, a, table, len, held, add);
+  if (not_ok || add == 0) {
+    if (not_ok && tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) report(c, not_ok, seq);
     return;
   }
   const int slot = len / R + blockIdx.x, base = slot * R;
   const int r0 = max(0, len - base), r1 = min(R, len + add - base);          // the page's new rows
   if (r0 < r1) {
-    const int page = table[slot];
-    unsigned char* to = c.pages + region(c, page, h, which) * (size_t)(R * D);
-    float* scale_p = c.scales + region(c, page, h, which);
+    const size_t reg = region(c, table[slot], h, which);
+    unsigned char* to = c.pages + reg * (size_t)(R * D);
     const Rows8& src = which ? a.v : a.k;
     const unsigned short* from = static_cast<const unsigned short*>(src.data) + i * src.batch + h * src.head;
-    const int pieces = (r1 - r0) * (D / 8);
-    Eight x[kPer];
+    const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2), pos0 = which == 0 && a.rot ? a.pos0[i] : 0;
+    Quad x;
     float most = 0.f;
     bool odd = false;
 #pragma unroll
-    for (int p = 0; p < kPer; ++p) {
-      const int at = tid + p * kRowThreads;
-      if (at < pieces) {
-        const int r = r0 + at / (D / 8), d = at % (D / 8) * 8, row = base + r - len;
-        const unsigned short* line = from + row * src.token;
-        x[p] = unpack8(*reinterpret_cast<const uint4*>(line + d), c.io);
-        if (which == 0 && d < a.rot) {
-          const int pos = a.pos0[i] + row, half = a.rot / 2;
-          if (a.pairs) {
+    for (int k = 0; k < 4; ++k) {
+      const int r = quad_row(blk, t, k), row = base + r - len;
+      if (r >= r0 && r < r1) {
+        x.row[k] = new_row(a, from + row * src.token, d, pos0 + row, which == 0, c.io);
+        largest(x.row[k], most, odd);
+      } else {
 #pragma unroll
-            for (int e = 0; e < 8; e += 2)
-              if (d + e < a.rot) {
-                float cs, sn;
-                turn_of(pos, a.turns[(d + e) / 2], cs, sn);
-                const float u = x[p].x[e], w = x[p].x[e + 1];
-                x[p].x[e] = a.amplitude * (u * cs - w * sn); x[p].x[e + 1] = a.amplitude * (u * sn + w * cs);
-              }
-          } else {
-            Eight y;
-            if (a.vec) y = unpack8(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)), c.io);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (d + e < a.rot) {
-                const bool lower = d + e < half;
-                if (!a.vec) y.x[e] = load16(line[lower ? d + e + half : d + e - half], c.io);
-                float cs, sn;
-                turn_of(pos, a.turns[lower ? d + e : d + e - half], cs, sn);
-                x[p].x[e] = a.amplitude * (lower ? x[p].x[e] * cs - y.x[e] * sn : y.x[e] * sn + x[p].x[e] * cs);
-              }
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float m = fabsf(x[p].x[e]);
-          if (m < INFINITY) most = fmaxf(most, m); else odd = true;
-        }
+        for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
       }
     }
     if (odd) report(c, kNotFinite, seq);
     int e = scale_exponent(block_max(most, warp_s), c.kind);
-    const int was = r0 ? exponent_of(*scale_p) : e;
-    e = max(e, was);
-    const float inv = pow2(-e);
-    if (r0 && e == was && pieces <= kRowThreads) {                           // a few rows beside others: straight to their places
-      if (tid < pieces) put8<D>(to, r0 + tid / (D / 8), tid % (D / 8) * 8, x[0], inv, which, c.kind);
-    } else {
-      if (r0) {
-        for (int q = tid; q < R * D / 16; q += kRowThreads) {
-          uint4 v = reinterpret_cast<const uint4*>(to)[q];
-          if (e != was) {
-            const float f = pow2(max(-126, was - e));
-            unsigned int* w = &v.x;
+    if (r0) {
+      const float old = c.scales[reg];
+      e = max(e, exponent_of(old));
+      const QuadWords w = get_words<D>(to, blk, t, d, which, r0);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const unsigned int o = w[k];
-              w[k] = code_pair(code_value(o & 0xFF, c.kind) * f, code_value(o >> 8 & 0xFF, c.kind) * f, c.kind) |
-                     code_pair(code_value(o >> 16 & 0xFF, c.kind) * f, code_value(o >> 24, c.kind) * f, c.kind) << 16;
-            }
-          }
-          reinterpret_cast<uint4*>(code_s)[q] = v;
-        }
-      } else if (r1 < R) {                                                   // rows without a value yet
-        for (int q = tid; q < R * D / 16; q += kRowThreads) reinterpret_cast<uint4*>(code_s)[q] = make_uint4(0, 0, 0, 0);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int p = 0; p < kPer; ++p) {
-        const int at = tid + p * kRowThreads;
-        if (at < pieces) put8<D>(code_s, r0 + at / (D / 8), at % (D / 8) * 8, x[p], inv, which, c.kind);
-      }
-      __syncthreads();
-      for (int q = tid; q < R * D / 16; q += kRowThreads) reinterpret_cast<uint4*>(to)[q] = reinterpret_cast<const uint4*>(code_s)[q];
+      for (int k = 0; k < 4; ++k) if (quad_row(blk, t, k) < r0) x.row[k] = row_of(w, k, old, which, c.kind);
+      __syncthreads();                                                       // the whole block has read the old scale
     }
-    if (tid == 0 && (!r0 || e != was)) *scale_p = pow2(e);
+    put_quad<D>(to, blk, t, d, x, pow2(-e), which, c.kind, 0, r1);
+    if (tid == 0) c.scales[reg] = pow2(e);
   }
   __syncthreads();                                                           // the whole block has read `len`
   if (tid == 0) {
@@ -269,35 +284,101 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
   }
 }
 
+// A few rows: a block a sequence, a warp for each head and tensor in turn, so that nothing waits on other blocks.  Only what holds
+// a new row is written, the whole page where its scale grows.  Latency: four dependent rounds of loads.  grid (n).
+constexpr int kFewWarps = 16;
+template <int D, int R>
+__global__ void __launch_bounds__(kFewWarps * 32)
+append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
+  const int lane = threadIdx.x & 31, i = blockIdx.x, seq = a.first + i * a.step;
+  pdl_launch();
+  pdl_wait();
+  const int len = c.len[seq], held = c.held[seq], add = a.rows ? a.rows[i] : a.cap;
+  const int* table = c.table + (size_t)seq * c.max_pages;
+  const int not_ok = no_room(c, a, table, len, held, add);
+  if (not_ok || add == 0) {
+    if (not_ok && threadIdx.x == 0) report(c, not_ok, seq);
+    return;
+  }
+  for (int base = len / R * R; base < len + add; base += R) {
+    const int page = table[base / R], r0 = max(0, len - base), r1 = min(R, len + add - base);
+    for (int hw = threadIdx.x >> 5; hw < 2 * c.Hkv; hw += blockDim.x >> 5) {
+      const int h = hw >> 1, which = hw & 1, pos0 = which == 0 && a.rot ? a.pos0[i] : 0;
+      const size_t reg = region(c, page, h, which);
+      unsigned char* to = c.pages + reg * (size_t)(R * D);
+      const Rows8& src = which ? a.v : a.k;
+      const unsigned short* from = static_cast<const unsigned short*>(src.data) + i * src.batch + h * src.head;
+      const float old = c.scales[reg];
+      float most = 0.f;
+      bool odd = false;
+      for (int p = lane; p < (r1 - r0) * (D / 8); p += 32) {
+        const int row = base + r0 + p / (D / 8) - len;
+        largest(new_row(a, from + row * src.token, p % (D / 8) * 8, pos0 + row, which == 0, c.io), most, odd);
+      }
+      if (odd) report(c, kNotFinite, seq);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+      int e = scale_exponent(most, c.kind);
+      const bool grows = !r0 || e > exponent_of(old);
+      e = grows ? e : exponent_of(old);
+      for (int u = lane; u < R * D / 32; u += 32) {
+        const int d = u % (D / 8) * 8, t = u / (D / 8) % 4, blk = u / (D / 2);
+        bool fresh = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) fresh |= quad_row(blk, t, k) >= r0 && quad_row(blk, t, k) < r1;
+        if (!fresh && !(grows && quad_row(blk, t, 0) < r0)) continue;        // row 0 is a quad's lowest
+        Quad x;
+        QuadWords w;
+        if (r0) w = get_words<D>(to, blk, t, d, which, r0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = quad_row(blk, t, k), row = base + r - len;
+          if (r < r0) x.row[k] = row_of(w, k, old, which, c.kind);
+          else if (r < r1) x.row[k] = new_row(a, from + row * src.token, d, pos0 + row, which == 0, c.io);
+          else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x.row[k].x[q] = 0.f;
+          }
+        }
+        put_quad<D>(to, blk, t, d, x, pow2(-e), which, c.kind, grows ? 0 : r0, r1);
+      }
+      __syncwarp();                                                          // every lane has read the old scale
+      if (lane == 0 && grows) c.scales[reg] = pow2(e);
+    }
+  }
+  __syncthreads();                                                           // the whole block has read `len`
+  if (threadIdx.x == 0) c.len[seq] = len + add;
+}
+
 // ---- rows out -----------------------------------------------------------------------------------------------------------
 
 struct ReadArgs { Rows8 k, v; int first, step, cap; };
 
-// The rows of one page, head and tensor as 16-bit numbers; rows past the sequence's length are not written.  Bound by HBM.
-// grid (pages of `cap` rows, 2 Hkv, n).
+// The rows of one page, head and tensor as 16-bit numbers, a quad a thread; rows past the sequence's length are not written.
+// Bound by HBM.  grid (pages of `cap` rows, 2 Hkv, n).
 template <int D, int R>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(R * D / 32)
 read8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ ReadArgs a) {
-  __shared__ __align__(16) unsigned char code_s[R * D];
   const int tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
+  const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   pdl_launch();
   pdl_wait();
   const int base = blockIdx.x * R, rows = min(R, min(c.len[seq], a.cap) - base);
   if (rows <= 0) return;
-  const int page = c.table[(size_t)seq * c.max_pages + blockIdx.x];
-  const uint4* from = reinterpret_cast<const uint4*>(c.pages + region(c, page, h, which) * (size_t)(R * D));
-  const float scale = c.scales[region(c, page, h, which)];
-  for (int q = tid; q < R * D / 16; q += kRowThreads) reinterpret_cast<uint4*>(code_s)[q] = from[q];
-  __syncthreads();
+  const size_t reg = region(c, c.table[(size_t)seq * c.max_pages + blockIdx.x], h, which);
+  const QuadWords w = get_words<D>(c.pages + reg * (size_t)(R * D), blk, t, d, which, rows);
+  const float scale = c.scales[reg];
   const Rows8& dst = which ? a.v : a.k;
-  unsigned short* to = static_cast<unsigned short*>(const_cast<void*>(dst.data)) + i * dst.batch + h * dst.head;
-  for (int at = tid; at < rows * (D / 8); at += kRowThreads) {
-    const int r = at / (D / 8), d = at % (D / 8) * 8;
-    const Eight e = get8<D>(code_s, r, d, scale, which, c.kind);
-    unsigned int w[4];
+  unsigned short* to = static_cast<unsigned short*>(const_cast<void*>(dst.data)) + i * dst.batch + h * dst.head + d;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = store16(e.x[2 * k], c.io) | store16(e.x[2 * k + 1], c.io) << 16;
-    *reinterpret_cast<uint4*>(to + (base + r) * dst.token + d) = make_uint4(w[0], w[1], w[2], w[3]);
+  for (int k = 0; k < 4; ++k) {
+    const int r = quad_row(blk, t, k);
+    if (r >= rows) continue;
+    const Eight e = row_of(w, k, scale, which, c.kind);
+    unsigned int o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] = store16(e.x[2 * q], c.io) | store16(e.x[2 * q + 1], c.io) << 16;
+    *reinterpret_cast<uint4*>(to + (base + r) * dst.token) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -506,58 +587,55 @@ struct CompactArgs {
 };
 
 // One page, head and tensor of a compacted sequence: row j is row idx[j] of the sequence as it is; a new page takes the scale
-// that its rows need.  grid (pages of `cols` rows, 2 Hkv, n).
+// that its rows need.  A quad a thread.  A row's values lie in 32 bytes of every 128, so four times their bytes are read.
+// grid (pages of `cols` rows, 2 Hkv, n).
 template <int D, int R>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(R * D / 32)
 compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ CompactArgs a) {
-  constexpr int kPieces = R * D / 8, kPer = (kPieces + kRowThreads - 1) / kRowThreads;
-  __shared__ __align__(16) unsigned char code_s[R * D];
-  __shared__ float warp_s[kRowThreads / 32];
-  __shared__ int idx_s[R];
+  __shared__ float warp_s[R * D / 1024];
   const int tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
+  const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   pdl_launch();
   pdl_wait();
   if ((int)blockIdx.x >= a.new_held[seq]) return;
   const int len = c.len[seq], base = blockIdx.x * R, rows = min(R, (a.count ? a.count[i] : a.cols) - base);
   const int* table = c.table + (size_t)seq * c.max_pages;
-  for (int r = tid; r < rows; r += kRowThreads) {
-    const int p = a.idx[((size_t)i * c.Hkv + h) * a.cols + base + r];
-    const bool bad = p < 0 || p >= len;
-    if (bad) report(c, kBadArgument, seq);
-    idx_s[r] = bad ? -1 : p;
+  const int* idx = a.idx + ((size_t)i * c.Hkv + h) * a.cols + base;
+  int from[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) from[k] = quad_row(blk, t, k) < rows ? idx[quad_row(blk, t, k)] : -1;
+  size_t reg[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const bool inside = from[k] >= 0 && from[k] < len;
+    if (!inside && quad_row(blk, t, k) < rows) report(c, kBadArgument, seq);
+    if (!inside) from[k] = -1;
+    reg[k] = inside ? region(c, table[from[k] / R], h, which) : 0;
   }
-  __syncthreads();
-  Eight x[kPer];
+  Quad x;
   float most = 0.f;
 #pragma unroll
-  for (int p = 0; p < kPer; ++p) {
-    const int at = tid + p * kRowThreads;
-    if (at < rows * (D / 8)) {
-      const int from = idx_s[at / (D / 8)], d = at % (D / 8) * 8;
-      if (from >= 0) {
-        const size_t reg = region(c, table[from / R], h, which);
-        x[p] = get8<D>(c.pages + reg * (size_t)(R * D), from % R, d, c.scales[reg], which, c.kind);
-      } else {
+  for (int k = 0; k < 4; ++k) {
+    if (from[k] < 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[p].x[e] = 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[p].x[e]));
+      for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
+      continue;
     }
+    const unsigned char* at = c.pages + reg[k] * (size_t)(R * D);
+    const int r = from[k] % R;
+    QuadWords w;
+    if (which) w = get_words<D>(at, r >> 4, (r & 7) >> 1, d, 1, R);
+    else w.v[0] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
+    x.row[k] = row_of(w, which ? (r & 1) + 2 * (r >> 3 & 1) : 0, c.scales[reg[k]], which, c.kind);
   }
-  if (rows < R)
-    for (int q = tid; q < R * D / 16; q += kRowThreads) reinterpret_cast<uint4*>(code_s)[q] = make_uint4(0, 0, 0, 0);
-  const int e = scale_exponent(block_max(most, warp_s), c.kind);             // (a barrier: the zeros above are in place)
 #pragma unroll
-  for (int p = 0; p < kPer; ++p) {
-    const int at = tid + p * kRowThreads;
-    if (at < rows * (D / 8)) put8<D>(code_s, at / (D / 8), at % (D / 8) * 8, x[p], pow2(-e), which, c.kind);
-  }
-  __syncthreads();
-  const size_t reg = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, which);
-  uint4* to = reinterpret_cast<uint4*>(c.pages + reg * (size_t)(R * D));
-  for (int q = tid; q < R * D / 16; q += kRowThreads) to[q] = reinterpret_cast<const uint4*>(code_s)[q];
-  if (tid == 0) c.scales[reg] = pow2(e);
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
+  const int e = scale_exponent(block_max(most, warp_s), c.kind);
+  const size_t to = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, which);
+  put_quad<D>(c.pages + to * (size_t)(R * D), blk, t, d, x, pow2(-e), which, c.kind, 0, rows);
+  if (tid == 0) c.scales[to] = pow2(e);
 }
 
 // The compacted sequences take the place of the old ones.  grid (n).
