@@ -110,7 +110,6 @@ int free_cache(dkv_cache8* c) {
   return DKV_OK;
 }
 
-constexpr int kFewRows = 8;                    // rows a call and sequence up to which a block takes a whole sequence (append8_few_kernel)
 constexpr int kMostQueries = 64;               // query rows of a KV head
 
 int attend_blocks(const dkv_cache8* c) { return std::min(c->n_sms, 256); }
@@ -307,6 +306,10 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   }
   TRY(cudaStreamSynchronize(cudaStreamLegacy));
   TRY(cfg->head_dim == 64 ? set_attend_smem<64>(cfg->kind) : set_attend_smem<128>(cfg->kind));
+  TRY(with_shape(c, [](auto d, auto r) {         // angles of a page's rows: the most that a head has
+    constexpr int D = decltype(d)::value, rows = decltype(r)::value;
+    return cudaFuncSetAttribute(append8_kernel<D, rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows * D / 2 * (int)sizeof(float2));
+  }));
 #undef TRY
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -328,9 +331,7 @@ int dkv_cache8_reserve(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   if (!aligned(rows, 4) || (!rows && add < 0)) return DKV_ERR_INVALID_ARG;
   if (n == 0) return DKV_OK;
   PlanArgs a = {rows, c->d_prefix, c->d_pick, c->d_jobs, nullptr, nullptr, first, step, n, add};
-  C8_LAUNCH(c, launch_pdl(plan_pages_kernel<false>, dim3(1), kPlanThreads, 0, 1, as_stream(stream), c->view, a));
-  const long long pieces = (long long)n * c->cfg.n_kv_heads * 2;
-  C8_LAUNCH(c, launch_pdl(copy_pages_kernel, dim3((unsigned)std::min(pieces, 2ll * c->n_sms)), kCopyThreads, 0, 1, as_stream(stream), c->view, (const int*)c->d_jobs));
+  C8_LAUNCH(c, launch_pdl(reserve8_kernel, dim3(kPlanBlocks), kPlanThreads, 0, kPlanBlocks, as_stream(stream), c->view, a));
   return DKV_OK;
 }
 
@@ -349,10 +350,14 @@ int dkv_cache8_append(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
     memcpy(a.turns, rotary->turns, sizeof a.turns);
   }
   const int R = c->cfg.page_rows, pages = (int)std::min<long long>(((long long)k->tokens + R - 2) / R + 1, c->cfg.max_pages);
+  // Heads and tensors a block: as many as leave four blocks an SM.
+  const long long blocks = 2ll * c->cfg.n_kv_heads * pages * n;
+  a.per = (int)std::min<long long>(2 * c->cfg.n_kv_heads, std::max(1ll, blocks / (4 * c->n_sms)));
   C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
     constexpr int D = decltype(d)::value, rows = decltype(r)::value;
     if (k->tokens <= kFewRows) return launch_pdl(append8_few_kernel<D, rows>, dim3(n), std::min(2 * c->cfg.n_kv_heads, kFewWarps) * 32, 0, 1, as_stream(stream), c->view, a);
-    return launch_pdl(append8_kernel<D, rows>, dim3(pages, 2 * c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, as_stream(stream), c->view, a);
+    return launch_pdl(append8_kernel<D, rows>, dim3(pages, (2 * c->cfg.n_kv_heads + a.per - 1) / a.per, n), rows * D / 32, (size_t)rows * a.rot / 2 * sizeof(float2), 1,
+                      as_stream(stream), c->view, a);
   }));
   return DKV_OK;
 }
@@ -417,12 +422,12 @@ int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   const PlanArgs p = {count, c->d_prefix, c->d_pick, c->d_jobs, c->d_new_table, c->d_new_held, first, step, n, cols};
   const CompactArgs a = {idx, count, c->d_new_table, c->d_new_held, first, step, cols};
   cudaStream_t st = as_stream(stream);
-  C8_LAUNCH(c, launch_pdl(plan_pages_kernel<true>, dim3(1), kPlanThreads, 0, 1, st, c->view, p));
+  C8_LAUNCH(c, launch_pdl(plan_compact8_kernel, dim3(1), kPlanThreads, 0, 1, st, c->view, p));
   const int R = c->cfg.page_rows, pages = std::min((int)(((long long)cols + R - 1) / R), c->cfg.max_pages);
   if (pages)
     C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
       constexpr int D = decltype(d)::value, rows = decltype(r)::value;
-      return launch_pdl(compact8_kernel<D, rows>, dim3(pages, 2 * c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, st, c->view, a);
+      return launch_pdl(compact8_kernel<D, rows>, dim3(pages, c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, st, c->view, a);
     }));
   C8_LAUNCH(c, launch_pdl(install8_kernel, dim3(n), kSeqThreads, 0, 1, st, c->view, a));
   return DKV_OK;

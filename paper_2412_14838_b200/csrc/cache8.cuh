@@ -135,6 +135,23 @@ __device__ __forceinline__ void put_quad(unsigned char* at, int blk, int t, int 
     }
   }
 }
+// Codes of eight dims of one row; other rows' codes stay.
+template <int D>
+__device__ __forceinline__ void put_row(unsigned char* at, int r, int d, const Eight& x, float inv, int which, int kind) {
+  unsigned int c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = code_pair(x.x[2 * i] * inv, x.x[2 * i + 1] * inv, kind);
+  if (which == 0) {
+    *reinterpret_cast<uint2*>(at + key_at<D>(r, d)) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+  } else {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      unsigned char* w = at + quad_values_at<D>(r >> 4, (r & 7) >> 1, d, p) + (r >> 3 & 1) * 2 + (r & 1);
+      const int i = 4 * (p >> 1) + (p & 1);
+      w[0] = (unsigned char)(c[i >> 1] >> (i & 1) * 8); w[4] = (unsigned char)(c[(i + 2) >> 1] >> (i & 1) * 8);
+    }
+  }
+}
 __device__ __forceinline__ Eight eight_of(unsigned int lo, unsigned int hi, float scale, int kind) {
   Eight e;
 #pragma unroll
@@ -171,41 +188,42 @@ struct AppendArgs {
   const int* rows;           // [n] rows of every sequence, or null: `cap` each
   const int* pos0;           // [n] position of the first new key, where keys are turned
   unsigned int* tickets;     // [n], zero between launches
-  int first, step, cap;
+  int first, step, cap, per;  // per: heads and tensors a block
   int rot, pairs, vec;       // vec: rot/2 is a multiple of 8 (a piece's partner is a piece)
   float amplitude;
   double turns[128];
 };
 
-// Eight dims of a new row; keys are turned where the call says so.
-__device__ __forceinline__ Eight new_row(const AppendArgs& a, const unsigned short* line, int d, int pos, bool turn, int io) {
-  Eight x = unpack8(*reinterpret_cast<const uint4*>(line + d), io);
-  if (turn && d < a.rot) {
-    const int half = a.rot / 2;
-    if (a.pairs) {
+// Turns eight dims d.. of a row; cs(i) gives (A cos, A sin) of pair i.
+template <typename F>
+__device__ __forceinline__ void turn_row(Eight& x, const AppendArgs& a, const unsigned short* line, int d, int io, F cs) {
+  if (d >= a.rot) return;
+  const int half = a.rot / 2;
+  if (a.pairs) {
 #pragma unroll
-      for (int e = 0; e < 8; e += 2)
-        if (d + e < a.rot) {
-          float cs, sn;
-          turn_of(pos, a.turns[(d + e) / 2], cs, sn);
-          const float u = x.x[e], w = x.x[e + 1];
-          x.x[e] = a.amplitude * (u * cs - w * sn); x.x[e + 1] = a.amplitude * (u * sn + w * cs);
-        }
-    } else {
-      Eight y;
-      if (a.vec) y = unpack8(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)), io);
+    for (int e = 0; e < 8; e += 2)
+      if (d + e < a.rot) {
+        const float2 f = cs((d + e) / 2);
+        const float u = x.x[e], w = x.x[e + 1];
+        x.x[e] = u * f.x - w * f.y; x.x[e + 1] = u * f.y + w * f.x;
+      }
+  } else {
+    Eight y;
+    if (a.vec) y = unpack8(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)), io);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (d + e < a.rot) {
-          const bool lower = d + e < half;
-          if (!a.vec) y.x[e] = load16(line[lower ? d + e + half : d + e - half], io);
-          float cs, sn;
-          turn_of(pos, a.turns[lower ? d + e : d + e - half], cs, sn);
-          x.x[e] = a.amplitude * (lower ? x.x[e] * cs - y.x[e] * sn : y.x[e] * sn + x.x[e] * cs);
-        }
-    }
+    for (int e = 0; e < 8; ++e)
+      if (d + e < a.rot) {
+        const bool lower = d + e < half;
+        if (!a.vec) y.x[e] = load16(line[lower ? d + e + half : d + e - half], io);
+        const float2 f = cs(lower ? d + e : d + e - half);
+        x.x[e] = lower ? x.x[e] * f.x - y.x[e] * f.y : y.x[e] * f.y + x.x[e] * f.x;
+      }
   }
-  return x;
+}
+__device__ __forceinline__ float2 turned_by(const AppendArgs& a, int pos, int pair) {
+  float c, s;
+  turn_of(pos, a.turns[pair], c, s);
+  return make_float2(a.amplitude * c, a.amplitude * s);
 }
 __device__ __forceinline__ void largest(const Eight& x, float& most, bool& odd) {
 #pragma unroll
@@ -221,15 +239,20 @@ __device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, con
   return add > 0 && len % c.R && c.refs[table[len / c.R]] != 1 ? kNoRoom : 0;
 }
 
-// Many rows: the new rows of one page, head and tensor.  Their largest magnitude gives the scale; where the page held rows before,
-// the old scale is a lower bound for it and the old codes are rounded again.  A thread has one quad, from 16-bit numbers in
-// registers straight to codes.  Bound by HBM (2 bytes in, 1 out).  grid (pages a sequence can touch, 2 Hkv, n); the last block
-// of a sequence to arrive (a ticket) makes the rows part of it.
+// Many rows: the new rows of one page, `per` heads and tensors one after the other.  Their largest magnitude gives the scale; where
+// the page held rows before, the old scale is a lower bound for it and the old codes are rounded again.  A thread has one quad, from
+// 16-bit numbers in registers straight to codes, and asks for the next one's rows before it works on this one's.  Bound by HBM (2
+// bytes in, 1 out), but for the chain of loads at a block's start and the ticket at its end, which is why a block has several heads
+// where there are blocks enough.  Angles are shared by all heads (shared memory, [R][rot/2]).  grid (pages a sequence can touch,
+// 2 Hkv / per, n); the last block of a sequence to arrive (a ticket) makes the rows part of it.
 template <int D, int R>
 __global__ void __launch_bounds__(R * D / 32)
 append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
-  __shared__ float warp_s[R * D / 1024];
-  const int tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
+  constexpr int kThreads = R * D / 32;
+  extern __shared__ float2 turn_s[];
+  __shared__ float warp_s[2][kThreads / 32];
+  const int tid = threadIdx.x, i = blockIdx.z, seq = a.first + i * a.step;
+  const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   pdl_launch();
   pdl_wait();
   const int len = c.len[seq], held = c.held[seq], add = a.rows ? a.rows[i] : a.cap;
@@ -242,37 +265,56 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
   const int slot = len / R + blockIdx.x, base = slot * R;
   const int r0 = max(0, len - base), r1 = min(R, len + add - base);          // the page's new rows
   if (r0 < r1) {
-    const size_t reg = region(c, table[slot], h, which);
-    unsigned char* to = c.pages + reg * (size_t)(R * D);
-    const Rows8& src = which ? a.v : a.k;
-    const unsigned short* from = static_cast<const unsigned short*>(src.data) + i * src.batch + h * src.head;
-    const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2), pos0 = which == 0 && a.rot ? a.pos0[i] : 0;
-    Quad x;
-    float most = 0.f;
-    bool odd = false;
+    const int page = table[slot], y0 = blockIdx.y * a.per, y1 = min(2 * c.Hkv, y0 + a.per);
+    struct Raw { uint4 v[4]; };
+    auto line = [&](int y, int k) {                                          // a new row of the source
+      const Rows8& src = y & 1 ? a.v : a.k;
+      return static_cast<const unsigned short*>(src.data) + i * src.batch + (y >> 1) * src.head + (base + quad_row(blk, t, k) - len) * src.token;
+    };
+    auto is_new = [&](int k) { return quad_row(blk, t, k) >= r0 && quad_row(blk, t, k) < r1; };
+    auto ask = [&](int y) {
+      Raw raw;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = quad_row(blk, t, k), row = base + r - len;
-      if (r >= r0 && r < r1) {
-        x.row[k] = new_row(a, from + row * src.token, d, pos0 + row, which == 0, c.io);
-        largest(x.row[k], most, odd);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
+      for (int k = 0; k < 4; ++k) raw.v[k] = is_new(k) ? *reinterpret_cast<const uint4*>(line(y, k) + d) : make_uint4(0, 0, 0, 0);
+      return raw;
+    };
+    Raw raw = ask(y0);
+    if (a.rot) {
+      const int pos0 = a.pos0[i] + base - len;
+      for (int x = tid; x < (r1 - r0) * (a.rot / 2); x += kThreads) {
+        const int r = r0 + x / (a.rot / 2), pair = x % (a.rot / 2);
+        turn_s[r * (a.rot / 2) + pair] = turned_by(a, pos0 + r, pair);
       }
+      __syncthreads();
     }
-    if (odd) report(c, kNotFinite, seq);
-    int e = scale_exponent(block_max(most, warp_s), c.kind);
-    if (r0) {
-      const float old = c.scales[reg];
-      e = max(e, exponent_of(old));
-      const QuadWords w = get_words<D>(to, blk, t, d, which, r0);
+    for (int y = y0; y < y1; ++y) {
+      const int which = y & 1;
+      const size_t reg = region(c, page, y >> 1, which);
+      unsigned char* to = c.pages + reg * (size_t)(R * D);
+      const Raw now = raw;
+      if (y + 1 < y1) raw = ask(y + 1);
+      Quad x;
+      float most = 0.f;
+      bool odd = false;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) if (quad_row(blk, t, k) < r0) x.row[k] = row_of(w, k, old, which, c.kind);
-      __syncthreads();                                                       // the whole block has read the old scale
+      for (int k = 0; k < 4; ++k) {
+        x.row[k] = unpack8(now.v[k], c.io);
+        if (a.rot && !which && is_new(k)) turn_row(x.row[k], a, line(y, k), d, c.io, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
+        largest(x.row[k], most, odd);
+      }
+      if (odd) report(c, kNotFinite, seq);
+      int e = scale_exponent(block_max(most, warp_s[y & 1]), c.kind);
+      if (r0) {
+        const float old = c.scales[reg];
+        e = max(e, exponent_of(old));
+        const QuadWords w = get_words<D>(to, blk, t, d, which, r0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (quad_row(blk, t, k) < r0) x.row[k] = row_of(w, k, old, which, c.kind);
+        __syncthreads();                                                     // the whole block has read the old scale
+      }
+      put_quad<D>(to, blk, t, d, x, pow2(-e), which, c.kind, 0, r1);
+      if (tid == 0) c.scales[reg] = pow2(e);
     }
-    put_quad<D>(to, blk, t, d, x, pow2(-e), which, c.kind, 0, r1);
-    if (tid == 0) c.scales[reg] = pow2(e);
   }
   __syncthreads();                                                           // the whole block has read `len`
   if (tid == 0) {
@@ -284,70 +326,86 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
   }
 }
 
-// A few rows: a block a sequence, a warp for each head and tensor in turn, so that nothing waits on other blocks.  Only what holds
-// a new row is written, the whole page where its scale grows.  Latency: four dependent rounds of loads.  grid (n).
-constexpr int kFewWarps = 16;
+// A few rows (at most kFewRows): a block a sequence, a warp for each head and tensor in turn, so that nothing waits on other blocks.
+// Latency: the new rows are on their way while the sequence's length, its table and the page's scale are looked up one after the
+// other; then every lane writes its eight codes of a row.  Only where the scale of a page with rows grows is the page read.  grid (n).
+constexpr int kFewRows = 8, kFewWarps = 16;
 template <int D, int R>
 __global__ void __launch_bounds__(kFewWarps * 32)
 append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
+  constexpr int kPer = kFewRows * D / 256;                                   // pieces (a row, eight dims) of a lane
   const int lane = threadIdx.x & 31, i = blockIdx.x, seq = a.first + i * a.step;
   pdl_launch();
   pdl_wait();
   const int len = c.len[seq], held = c.held[seq], add = a.rows ? a.rows[i] : a.cap;
   const int* table = c.table + (size_t)seq * c.max_pages;
-  const int not_ok = no_room(c, a, table, len, held, add);
-  if (not_ok || add == 0) {
-    if (not_ok && threadIdx.x == 0) report(c, not_ok, seq);
-    return;
-  }
-  for (int base = len / R * R; base < len + add; base += R) {
-    const int page = table[base / R], r0 = max(0, len - base), r1 = min(R, len + add - base);
-    for (int hw = threadIdx.x >> 5; hw < 2 * c.Hkv; hw += blockDim.x >> 5) {
-      const int h = hw >> 1, which = hw & 1, pos0 = which == 0 && a.rot ? a.pos0[i] : 0;
-      const size_t reg = region(c, page, h, which);
+  bool ok = true;
+  for (int hw = threadIdx.x >> 5; ok && hw < 2 * c.Hkv; hw += blockDim.x >> 5) {
+    const int h = hw >> 1, which = hw & 1;
+    const Rows8& src = which ? a.v : a.k;
+    const unsigned short* from = static_cast<const unsigned short*>(src.data) + i * src.batch + h * src.head;
+    Eight x[kPer];
+    uint4 raw[kPer];
+#pragma unroll
+    for (int p = 0; p < kPer; ++p) {
+      const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8;
+      raw[p] = j < a.cap ? *reinterpret_cast<const uint4*>(from + j * src.token + d) : make_uint4(0, 0, 0, 0);
+    }
+    const int pos0 = a.rot && !which ? a.pos0[i] : 0;
+    const int not_ok = no_room(c, a, table, len, held, add);
+    if (not_ok || add == 0) {
+      if (not_ok && threadIdx.x == 0) report(c, not_ok, seq);
+      ok = false;
+      break;
+    }
+#pragma unroll
+    for (int p = 0; p < kPer; ++p) {
+      const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8;
+      x[p] = unpack8(raw[p], c.io);
+      if (a.rot && !which && j < add) turn_row(x[p], a, from + j * src.token, d, c.io, [&](int pair) { return turned_by(a, pos0 + j, pair); });
+    }
+    for (int base = len / R * R; base < len + add; base += R) {
+      const int r0 = max(0, len - base), r1 = min(R, len + add - base);
+      const size_t reg = region(c, table[base / R], h, which);
       unsigned char* to = c.pages + reg * (size_t)(R * D);
-      const Rows8& src = which ? a.v : a.k;
-      const unsigned short* from = static_cast<const unsigned short*>(src.data) + i * src.batch + h * src.head;
       const float old = c.scales[reg];
       float most = 0.f;
       bool odd = false;
-      for (int p = lane; p < (r1 - r0) * (D / 8); p += 32) {
-        const int row = base + r0 + p / (D / 8) - len;
-        largest(new_row(a, from + row * src.token, p % (D / 8) * 8, pos0 + row, which == 0, c.io), most, odd);
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        const int j = (lane + 32 * p) / (D / 8), r = len + j - base;
+        if (j < add && r >= r0 && r < r1) largest(x[p], most, odd);
       }
       if (odd) report(c, kNotFinite, seq);
 #pragma unroll
       for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
       int e = scale_exponent(most, c.kind);
-      const bool grows = !r0 || e > exponent_of(old);
-      e = grows ? e : exponent_of(old);
-      for (int u = lane; u < R * D / 32; u += 32) {
-        const int d = u % (D / 8) * 8, t = u / (D / 8) % 4, blk = u / (D / 2);
-        bool fresh = false;
+      if (r0 && e > exponent_of(old)) {                                      // the page's older codes are rounded again
+        for (int u = lane; u < R * D / 32; u += 32) {
+          const int d = u % (D / 8) * 8, t = u / (D / 8) % 4, blk = u / (D / 2);
+          if (quad_row(blk, t, 0) >= r0) continue;                           // (row 0 is a quad's lowest)
+          const QuadWords w = get_words<D>(to, blk, t, d, which, r0);
+          Quad q;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) fresh |= quad_row(blk, t, k) >= r0 && quad_row(blk, t, k) < r1;
-        if (!fresh && !(grows && quad_row(blk, t, 0) < r0)) continue;        // row 0 is a quad's lowest
-        Quad x;
-        QuadWords w;
-        if (r0) w = get_words<D>(to, blk, t, d, which, r0);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int r = quad_row(blk, t, k), row = base + r - len;
-          if (r < r0) x.row[k] = row_of(w, k, old, which, c.kind);
-          else if (r < r1) x.row[k] = new_row(a, from + row * src.token, d, pos0 + row, which == 0, c.io);
-          else {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) x.row[k].x[q] = 0.f;
-          }
+          for (int k = 0; k < 4; ++k) q.row[k] = row_of(w, k, old, which, c.kind);
+          put_quad<D>(to, blk, t, d, q, pow2(-e), which, c.kind, 0, r0);
         }
-        put_quad<D>(to, blk, t, d, x, pow2(-e), which, c.kind, grows ? 0 : r0, r1);
+        __syncwarp();                                                        // the new rows share words with the old ones
+      } else if (r0) {
+        e = exponent_of(old);
+      }
+      const float inv = pow2(-e);
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8, r = len + j - base;
+        if (j < add && r >= r0 && r < r1) put_row<D>(to, r, d, x[p], inv, which, c.kind);
       }
       __syncwarp();                                                          // every lane has read the old scale
-      if (lane == 0 && grows) c.scales[reg] = pow2(e);
+      if (lane == 0 && (!r0 || e != exponent_of(old))) c.scales[reg] = pow2(e);
     }
   }
   __syncthreads();                                                           // the whole block has read `len`
-  if (threadIdx.x == 0) c.len[seq] = len + add;
+  if (threadIdx.x == 0 && ok) c.len[seq] = len + add;
 }
 
 // ---- rows out -----------------------------------------------------------------------------------------------------------
@@ -419,16 +477,13 @@ __device__ __forceinline__ long long block_scan(long long v, long long* warp_s, 
 // Pages for sequences that are to grow by count[i] rows (kCompact = false), or for the count[i] rows that a compaction keeps.
 // Free pages are given out lowest first, in the order of the sequences: what a call does depends on nothing but the state it
 // finds.  Where they do not last, the sequences from the first that cannot be served on get none.  A sequence that is to grow
-// and whose last page is only partly filled and held by others too gets a page of its own, to be filled by copy_pages_kernel.
-// One block: latency, a few us (one scan over the sequences, one over the words of `free` up to the last page given out).
+// and whose last page is only partly filled and held by others too gets a page of its own, to be filled with that page's rows.
+// One block plans: latency, a few us (one scan over the sequences, one over the words of `free` up to the last page given out).
 template <bool kCompact>
-__global__ void __launch_bounds__(kPlanThreads)
-plan_pages_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ PlanArgs a) {
+__device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
   __shared__ long long warp_s[32];
   __shared__ int jobs_s;
   const int tid = threadIdx.x;
-  pdl_launch();
-  pdl_wait();
   if (tid == 0) jobs_s = 0;
   auto own_copy = [&](int seq, int len) { return len % c.R && c.refs[c.table[(size_t)seq * c.max_pages + len / c.R]] > 1; };
   int all = 0;
@@ -518,21 +573,31 @@ plan_pages_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Plan
   if (!kCompact && tid == 0) a.jobs[0] = jobs_s;
 }
 
-// Pages that a sequence shared and is to write to: jobs[1 + 2 j] is copied to jobs[2 + 2 j], all heads.  Bound by HBM.
-constexpr int kCopyThreads = 256;
-__global__ void __launch_bounds__(kCopyThreads)
-copy_pages_kernel(const __grid_constant__ Cache8 c, const int* jobs) {
+// A cluster of kPlanBlocks: its first block plans, then all of them copy the pages that sequences shared and are to write to
+// (jobs[1 + 2 j] to jobs[2 + 2 j], all heads), mostly none: a launch of its own for that cost every step 2.4 us more.
+constexpr int kPlanBlocks = 8;
+__global__ void __launch_bounds__(kPlanThreads)
+reserve8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ PlanArgs a) {
   pdl_launch();
   pdl_wait();
-  const int n = jobs[0], regions = c.Hkv * 2, vec = c.R * c.D / 16;
-  for (long long at = blockIdx.x; at < (long long)n * regions; at += gridDim.x) {
-    const int j = (int)(at / regions), r = (int)(at % regions);
-    const size_t from = (size_t)jobs[1 + 2 * j] * regions + r, to = (size_t)jobs[2 + 2 * j] * regions + r;
+  if (blockIdx.x == 0) plan_pages<false>(c, a);
+  __threadfence();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  const int n = __ldcg(a.jobs);
+  const size_t vec = (size_t)c.Hkv * 2 * c.R * c.D / 16;                      // a page
+  for (int j = 0; j < n; ++j) {
+    const size_t from = __ldcg(a.jobs + 1 + 2 * j), to = __ldcg(a.jobs + 2 + 2 * j);
     const uint4* s = reinterpret_cast<const uint4*>(c.pages) + from * vec;
     uint4* d = reinterpret_cast<uint4*>(c.pages) + to * vec;
-    for (int q = threadIdx.x; q < vec; q += kCopyThreads) d[q] = s[q];
-    if (threadIdx.x == 0) c.scales[to] = c.scales[from];
+    for (size_t q = blockIdx.x * kPlanThreads + threadIdx.x; q < vec; q += kPlanBlocks * kPlanThreads) d[q] = s[q];
+    for (int r = blockIdx.x * kPlanThreads + threadIdx.x; r < c.Hkv * 2; r += kPlanBlocks * kPlanThreads) c.scales[to * c.Hkv * 2 + r] = c.scales[from * c.Hkv * 2 + r];
   }
+}
+__global__ void __launch_bounds__(kPlanThreads)
+plan_compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ PlanArgs a) {
+  pdl_launch();
+  pdl_wait();
+  plan_pages<true>(c, a);
 }
 
 // Gives back the pages [from, to) of a sequence's table.
@@ -586,56 +651,67 @@ struct CompactArgs {
   int first, step, cols;
 };
 
-// One page, head and tensor of a compacted sequence: row j is row idx[j] of the sequence as it is; a new page takes the scale
-// that its rows need.  A quad a thread.  A row's values lie in 32 bytes of every 128, so four times their bytes are read.
-// grid (pages of `cols` rows, 2 Hkv, n).
+// One page and head of a compacted sequence: row j is row idx[j] of the sequence as it is; a new page takes the scales that its rows
+// need.  A quad of keys and one of values a thread, all their loads in flight.  A row's values lie in 32 bytes of every 128, so four
+// times their bytes are read.  grid (pages of `cols` rows, Hkv, n).
 template <int D, int R>
 __global__ void __launch_bounds__(R * D / 32)
 compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ CompactArgs a) {
-  __shared__ float warp_s[R * D / 1024];
-  const int tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
+  __shared__ float warp_s[2][R * D / 1024];
+  const int tid = threadIdx.x, h = blockIdx.y, i = blockIdx.z, seq = a.first + i * a.step;
   const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
+  const int* idx = a.idx + ((size_t)i * c.Hkv + h) * a.cols + blockIdx.x * R;
   pdl_launch();
   pdl_wait();
-  if ((int)blockIdx.x >= a.new_held[seq]) return;
-  const int len = c.len[seq], base = blockIdx.x * R, rows = min(R, (a.count ? a.count[i] : a.cols) - base);
-  const int* table = c.table + (size_t)seq * c.max_pages;
-  const int* idx = a.idx + ((size_t)i * c.Hkv + h) * a.cols + base;
-  int from[4];
+  const int base = blockIdx.x * R;
+  int from[4];                                                               // asked for with what says how many count
 #pragma unroll
-  for (int k = 0; k < 4; ++k) from[k] = quad_row(blk, t, k) < rows ? idx[quad_row(blk, t, k)] : -1;
+  for (int k = 0; k < 4; ++k) from[k] = base + quad_row(blk, t, k) < a.cols ? idx[quad_row(blk, t, k)] : -1;
+  const int held = a.new_held[seq], len = c.len[seq], rows = min(R, (a.count ? a.count[i] : a.cols) - base);
+  if ((int)blockIdx.x >= held) return;
+  const int* table = c.table + (size_t)seq * c.max_pages;
   size_t reg[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const bool inside = from[k] >= 0 && from[k] < len;
-    if (!inside && quad_row(blk, t, k) < rows) report(c, kBadArgument, seq);
+    const bool wanted = quad_row(blk, t, k) < rows, inside = wanted && from[k] >= 0 && from[k] < len;
+    if (wanted && !inside) report(c, kBadArgument, seq);
     if (!inside) from[k] = -1;
-    reg[k] = inside ? region(c, table[from[k] / R], h, which) : 0;
+    reg[k] = inside ? region(c, table[from[k] / R], h, 0) : 0;
   }
-  Quad x;
-  float most = 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (from[k] < 0) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
-      continue;
-    }
-    const unsigned char* at = c.pages + reg[k] * (size_t)(R * D);
-    const int r = from[k] % R;
-    QuadWords w;
-    if (which) w = get_words<D>(at, r >> 4, (r & 7) >> 1, d, 1, R);
-    else w.v[0] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
-    x.row[k] = row_of(w, which ? (r & 1) + 2 * (r >> 3 & 1) : 0, c.scales[reg[k]], which, c.kind);
-  }
+  uint2 key[4];
+  QuadWords value[4];
+  float2 scale[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
+    if (from[k] >= 0) {
+      const unsigned char* at = c.pages + reg[k] * (size_t)(R * D);
+      const int r = from[k] % R;
+      key[k] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
+      value[k] = get_words<D>(at + R * D, r >> 4, (r & 7) >> 1, d, 1, R);
+      scale[k] = *reinterpret_cast<const float2*>(c.scales + reg[k]);
+    }
+  const size_t to = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, 0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
-  const int e = scale_exponent(block_max(most, warp_s), c.kind);
-  const size_t to = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, which);
-  put_quad<D>(c.pages + to * (size_t)(R * D), blk, t, d, x, pow2(-e), which, c.kind, 0, rows);
-  if (tid == 0) c.scales[to] = pow2(e);
+  for (int which = 0; which < 2; ++which) {
+    Quad x;
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (from[k] < 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
+      } else if (which == 0) {
+        x.row[k] = eight_of(key[k].x, key[k].y, scale[k].x, c.kind);
+      } else {
+        x.row[k] = row_of(value[k], (from[k] & 1) + 2 * (from[k] >> 3 & 1), scale[k].y, 1, c.kind);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
+    }
+    const int e = scale_exponent(block_max(most, warp_s[which]), c.kind);
+    put_quad<D>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(-e), which, c.kind, 0, rows);
+    if (tid == 0) c.scales[to + which] = pow2(e);
+  }
 }
 
 // The compacted sequences take the place of the old ones.  grid (n).
