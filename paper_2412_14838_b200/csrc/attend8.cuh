@@ -32,7 +32,7 @@ struct AttendArgs {
   float* lse;                // [n][Hq][nq] or null
   float* scratch;            // [2 slices][rows of a head, in whole QB] partial results, (reference, sum) behind them
   unsigned int* tickets;     // [n * Hkv], zero between launches
-  int first, step, n, nq, rows, G, causal, slots;
+  int first, step, n, nq, rows, G, causal, slots, io;
   float scale2;              // log2(e) / sqrt(D)
 };
 
@@ -103,7 +103,7 @@ struct AttendWarp {
         for (int e = 0; e < 2; ++e) raw.v[i][p][e] = there ? *reinterpret_cast<const uint4*>(from + p * 64 + e * 8) : make_uint4(0, 0, 0, 0);
     }
   }
-  __device__ __forceinline__ void start(const Raw& raw, const AttendArgs& a, int c0, int len, int io, int g) {
+  __device__ __forceinline__ void start(const Raw& raw, const AttendArgs& a, int c0, int len, int g) {
 #pragma unroll
     for (int i = 0; i < kHalves; ++i) {
       const int row = c0 + g + 8 * i;
@@ -113,7 +113,7 @@ struct AttendWarp {
       for (int p = 0; p < kPanels; ++p)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          x[p][e] = unpack8(raw.v[i][p][e], io);
+          x[p][e] = a.io == DKV_BF16 ? unpack8<DKV_BF16>(raw.v[i][p][e]) : unpack8<DKV_F16>(raw.v[i][p][e]);
 #pragma unroll
           for (int k = 0; k < 8; ++k) { most = fmaxf(most, fabsf(x[p][e].x[k])); none = fmaf(x[p][e].x[k], 0.f, none); }
         }
@@ -380,7 +380,7 @@ struct Ring {
     auto look = [&](int x0) {
       const int x = x0 + lane;
       if (x < count) {
-        page = table[(first + x * step * kAttendRows) / c.R];
+        page = table[(first + x * step * kAttendRows) >> c.shift];
         sc = *reinterpret_cast<const float2*>(c.scales + region(c, page, h, 0));
       }
     };
@@ -388,7 +388,7 @@ struct Ring {
       if (x >= count || broken) return;
       const int row = first + x * step * kAttendRows, p = __shfl_sync(0xFFFFFFFFu, page, x & 31);
       if (lane == 0) {
-        const unsigned char* k = c.pages + region(c, p, h, 0) * (size_t)(c.R * D) + (row % c.R) * D;
+        const unsigned char* k = c.pages + region(c, p, h, 0) * (size_t)(c.R * D) + (row & (c.R - 1)) * D;
         const uint32_t bar = bar_s + into * 8, to = at_s + into * kChunkBytes;
         ring_expect(bar, kChunkBytes);
         if (c.R == kAttendRows) ring_copy(to, k, kChunkBytes, bar);
@@ -398,7 +398,7 @@ struct Ring {
     look(0);
 #pragma unroll
     for (int x = 0; x < kAttendStages - 1; ++x) fetch(x, (stage + x) % kAttendStages);
-    w.start(raw, a, c0, len, c.io, g);
+    w.start(raw, a, c0, len, g);
     float2 now = sc;                                   // scales of the chunks being worked on (`sc` runs ahead)
     for (int x = 0; x < count; ++x) {
       if ((x & 31) == 0) now = sc;

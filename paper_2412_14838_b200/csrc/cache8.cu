@@ -147,18 +147,14 @@ bool fits(const dkv_cache8* c, const dkv_rows* r, int n, int heads) {
 }
 Rows8 rows8(const dkv_rows* r) { return {r->data, r->batch_stride, r->head_stride, r->token_stride}; }
 
-// Calls f with std::integral_constants of the cache's head size and page rows.
+// Calls f with std::integral_constants of the cache's head size, kind of codes and type of rows.
 template <typename F>
-cudaError_t with_shape(const dkv_cache8* c, F f) {
-  auto rows = [&](auto d) {
-    switch (c->cfg.page_rows) {
-      case 32: return f(d, std::integral_constant<int, 32>());
-      case 64: return f(d, std::integral_constant<int, 64>());
-      default: return f(d, std::integral_constant<int, 128>());
-    }
-  };
-  return c->cfg.head_dim == 64 ? rows(std::integral_constant<int, 64>()) : rows(std::integral_constant<int, 128>());
+cudaError_t with_types(const dkv_cache8* c, F f) {
+  auto types = [&](auto d, auto kind) { return c->cfg.io == DKV_BF16 ? f(d, kind, std::integral_constant<int, DKV_BF16>()) : f(d, kind, std::integral_constant<int, DKV_F16>()); };
+  auto kinds = [&](auto d) { return c->cfg.kind == DKV_E4M3 ? types(d, std::integral_constant<int, kE4m3>()) : types(d, std::integral_constant<int, kInt8>()); };
+  return c->cfg.head_dim == 64 ? kinds(std::integral_constant<int, 64>()) : kinds(std::integral_constant<int, 128>());
 }
+int quad_threads(const dkv_cache8* c) { return c->cfg.page_rows * c->cfg.head_dim / 32; }
 
 template <int D, int QB, int kKind>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
@@ -263,7 +259,7 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   c->cfg = *cfg;
   Cache8& v = c->view;
   v.Hkv = cfg->n_kv_heads; v.D = cfg->head_dim; v.R = cfg->page_rows; v.max_pages = cfg->max_pages; v.n_pages = cfg->n_pages;
-  v.kind = cfg->kind; v.io = cfg->io;
+  v.shift = cfg->page_rows == 32 ? 5 : cfg->page_rows == 64 ? 6 : 7;
   const size_t regions = (size_t)cfg->n_pages * cfg->n_kv_heads * 2, entries = (size_t)cfg->n_seqs * cfg->max_pages;
   const int words = (cfg->n_pages + 31) / 32;
   cudaError_t e = cudaGetDevice(&c->device);
@@ -306,9 +302,9 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   }
   TRY(cudaStreamSynchronize(cudaStreamLegacy));
   TRY(cfg->head_dim == 64 ? set_attend_smem<64>(cfg->kind) : set_attend_smem<128>(cfg->kind));
-  TRY(with_shape(c, [](auto d, auto r) {         // angles of a page's rows: the most that a head has
-    constexpr int D = decltype(d)::value, rows = decltype(r)::value;
-    return cudaFuncSetAttribute(append8_kernel<D, rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, rows * D / 2 * (int)sizeof(float2));
+  TRY(with_types(c, [](auto d, auto kind, auto io) {       // angles of a page's rows: the most that any cache has
+    return cudaFuncSetAttribute(append8_kernel<decltype(d)::value, decltype(kind)::value, decltype(io)::value>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                128 * decltype(d)::value / 2 * (int)sizeof(float2));
   }));
 #undef TRY
   if (e != cudaSuccess) {
@@ -353,10 +349,10 @@ int dkv_cache8_append(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   // Heads and tensors a block: as many as leave four blocks an SM.
   const long long blocks = 2ll * c->cfg.n_kv_heads * pages * n;
   a.per = (int)std::min<long long>(2 * c->cfg.n_kv_heads, std::max(1ll, blocks / (4 * c->n_sms)));
-  C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
-    constexpr int D = decltype(d)::value, rows = decltype(r)::value;
-    if (k->tokens <= kFewRows) return launch_pdl(append8_few_kernel<D, rows>, dim3(n), std::min(2 * c->cfg.n_kv_heads, kFewWarps) * 32, 0, 1, as_stream(stream), c->view, a);
-    return launch_pdl(append8_kernel<D, rows>, dim3(pages, (2 * c->cfg.n_kv_heads + a.per - 1) / a.per, n), rows * D / 32, (size_t)rows * a.rot / 2 * sizeof(float2), 1,
+  C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto io) {
+    constexpr int D = decltype(d)::value, K = decltype(kind)::value, I = decltype(io)::value;
+    if (k->tokens <= kFewRows) return launch_pdl(append8_few_kernel<D, K, I>, dim3(n), std::min(2 * c->cfg.n_kv_heads, kFewWarps) * 32, 0, 1, as_stream(stream), c->view, a);
+    return launch_pdl(append8_kernel<D, K, I>, dim3(pages, (2 * c->cfg.n_kv_heads + a.per - 1) / a.per, n), quad_threads(c), (size_t)R * a.rot / 2 * sizeof(float2), 1,
                       as_stream(stream), c->view, a);
   }));
   return DKV_OK;
@@ -368,9 +364,9 @@ int dkv_cache8_read(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const
   if (n == 0 || k_out->tokens == 0) return DKV_OK;
   const ReadArgs a = {rows8(k_out), rows8(v_out), first, step, k_out->tokens};
   const int R = c->cfg.page_rows, pages = std::min((int)(((long long)k_out->tokens + R - 1) / R), c->cfg.max_pages);
-  C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
-    constexpr int D = decltype(d)::value, rows = decltype(r)::value;
-    return launch_pdl(read8_kernel<D, rows>, dim3(pages, 2 * c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, as_stream(stream), c->view, a);
+  C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto io) {
+    return launch_pdl(read8_kernel<decltype(d)::value, decltype(kind)::value, decltype(io)::value>, dim3(pages, 2 * c->cfg.n_kv_heads, n), quad_threads(c), 0, 1,
+                      as_stream(stream), c->view, a);
   }));
   return DKV_OK;
 }
@@ -388,7 +384,7 @@ int dkv_cache8_attend(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   a.q_batch = q->batch_stride; a.q_head = q->head_stride; a.q_token = q->token_stride;
   a.out_batch = out->batch_stride; a.out_head = out->head_stride; a.out_token = out->token_stride;
   a.scratch = c->d_scratch; a.tickets = c->d_tickets;
-  a.step = step; a.nq = q->tokens; a.rows = G * q->tokens; a.G = G; a.causal = causal != 0;
+  a.step = step; a.nq = q->tokens; a.rows = G * q->tokens; a.G = G; a.causal = causal != 0; a.io = c->cfg.io;
   a.slots = (a.rows + (a.rows <= 8 ? 7 : 15)) / (a.rows <= 8 ? 8 : 16);
   a.scale2 = kLog2e / sqrtf((float)c->cfg.head_dim);
   // sequences a launch: their prefix sums fit shared memory, and their units (chunks, at most) 31 bits
@@ -425,9 +421,8 @@ int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   C8_LAUNCH(c, launch_pdl(plan_compact8_kernel, dim3(1), kPlanThreads, 0, 1, st, c->view, p));
   const int R = c->cfg.page_rows, pages = std::min((int)(((long long)cols + R - 1) / R), c->cfg.max_pages);
   if (pages)
-    C8_LAUNCH(c, with_shape(c, [&](auto d, auto r) {
-      constexpr int D = decltype(d)::value, rows = decltype(r)::value;
-      return launch_pdl(compact8_kernel<D, rows>, dim3(pages, c->cfg.n_kv_heads, n), rows * D / 32, 0, 1, st, c->view, a);
+    C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto) {
+      return launch_pdl(compact8_kernel<decltype(d)::value, decltype(kind)::value>, dim3(pages, c->cfg.n_kv_heads, n), quad_threads(c), 0, 1, st, c->view, a);
     }));
   C8_LAUNCH(c, launch_pdl(install8_kernel, dim3(n), kSeqThreads, 0, 1, st, c->view, a));
   return DKV_OK;

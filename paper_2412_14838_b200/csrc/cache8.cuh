@@ -35,7 +35,7 @@ struct Cache8 {
   unsigned int* free;        // bit per page: free
   int* hint;                 // no word of `free` before this one has a bit set
   int* status;               // [0] bits, [1] lowest sequence concerned
-  int Hkv, D, R, max_pages, n_pages, kind, io;
+  int Hkv, D, R, shift, max_pages, n_pages;     // R = 2^shift
 };
 
 __device__ __forceinline__ void report(const Cache8& c, int bit, int seq) {
@@ -57,35 +57,61 @@ __device__ __forceinline__ int scale_exponent(float most, int kind) {
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned int)(e + 127) << 23); }       // -126 <= e <= 127
 __device__ __forceinline__ int exponent_of(float s) { return (int)(__float_as_uint(s) >> 23) - 127; }          // of a power of two
 
-// Codes of two numbers already divided by their scale: clamped, nearest, ties to even, NaN as 0.
-__device__ __forceinline__ unsigned int code_pair(float a, float b, int kind) {
-  a = a == a ? a : 0.f; b = b == b ? b : 0.f;
-  if (kind == kE4m3) return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const int x = __float2int_rn(fminf(fmaxf(a, -127.f), 127.f)), y = __float2int_rn(fminf(fmaxf(b, -127.f), 127.f));
-  return (x + 128) | (y + 128) << 8;
+// Four numbers times inv, a power of two, as four codes: nearest, ties to even, beyond the largest the largest.  Not NaN; for int8
+// the products are at most 127 in magnitude.
+template <int kKind>
+__device__ __forceinline__ unsigned int word_of(float a, float b, float c, float d, float inv) {
+  if constexpr (kKind == kE4m3) {
+    const unsigned int x = __nv_cvt_float2_to_fp8x2(make_float2(a * inv, b * inv), __NV_SATFINITE, __NV_E4M3);
+    return x | (unsigned int)__nv_cvt_float2_to_fp8x2(make_float2(c * inv, d * inv), __NV_SATFINITE, __NV_E4M3) << 16;
+  } else {                   // 1.5 * 2^23 + 128 + product: a float's last bit is 1 there, its last byte the code
+    constexpr float off = 12582912.f + 128.f;
+    auto bits = [&](float x) { return __float_as_uint(fmaf(x, inv, off)); };
+    return __byte_perm(__byte_perm(bits(a), bits(b), 0x0040), __byte_perm(bits(c), bits(d), 0x0040), 0x5410);
+  }
 }
-__device__ __forceinline__ float code_value(unsigned int byte, int kind) {
-  if (kind == kInt8) return (float)((int)byte - 128);
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
+// Four codes as numbers, times scale.
+template <int kKind>
+__device__ __forceinline__ void values_of(unsigned int w, float scale, float* x) {
+  if constexpr (kKind == kE4m3) {
+    const __half2 lo = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFF), __NV_E4M3));
+    const __half2 hi = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3));
+    const float2 a = __half22float2(lo), b = __half22float2(hi);
+    x[0] = a.x * scale; x[1] = a.y * scale; x[2] = b.x * scale; x[3] = b.y * scale;
+  } else {                   // 2^23 + byte, less 2^23 + 128 (before the product, which a large scale would take beyond all floats)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + i)) - (8388608.f + 128.f)) * scale;
+  }
 }
 
-// A 16-bit number of the caller's type.
-__device__ __forceinline__ float load16(unsigned int bits, int io) {
-  return io == DKV_BF16 ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half((unsigned short)bits));
-}
-__device__ __forceinline__ unsigned int store16(float x, int io) {
-  if (io == DKV_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(fminf(fmaxf(x, -3.3895313892515355e38f), 3.3895313892515355e38f)));
-  return __half_as_ushort(__float2half_rn(fminf(fmaxf(x, -65504.f), 65504.f)));
-}
-
-// Eight numbers of one row.
+// Eight 16-bit numbers of the caller's type, and back.
 struct Eight { float x[8]; };
-__device__ __forceinline__ Eight unpack8(uint4 v, int io) {
+template <int kIo>
+__device__ __forceinline__ Eight unpack8(uint4 v) {
   Eight e;
   const unsigned int w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { e.x[2 * i] = load16(w[i] & 0xFFFF, io); e.x[2 * i + 1] = load16(w[i] >> 16, io); }
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kIo == DKV_BF16) { e.x[2 * i] = __uint_as_float(w[i] << 16); e.x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i])); e.x[2 * i] = f.x; e.x[2 * i + 1] = f.y; }
+  }
   return e;
+}
+template <int kIo>
+__device__ __forceinline__ float load16(unsigned short v) {
+  return kIo == DKV_BF16 ? __uint_as_float((unsigned int)v << 16) : __half2float(__ushort_as_half(v));
+}
+template <int kIo>
+__device__ __forceinline__ uint4 pack8(const Eight& e) {       // a code's value may pass the type's largest number by a rounding
+  unsigned int o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    constexpr float most = kIo == DKV_BF16 ? 3.3895313892515355e38f : 65504.f;
+    const float a = fminf(fmaxf(e.x[2 * i], -most), most), b = fminf(fmaxf(e.x[2 * i + 1], -most), most);
+    if constexpr (kIo == DKV_BF16) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); o[i] = *reinterpret_cast<const unsigned int*>(&h); }
+    else { const __half2 h = __floats2half2_rn(a, b); o[i] = *reinterpret_cast<const unsigned int*>(&h); }
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
 // Largest of a value per thread over the block.
@@ -107,56 +133,39 @@ __device__ __forceinline__ int quad_values_at(int blk, int t, int d, int pair) {
   const int g = 2 * ((d & 15) >> 2) + pair;
   return blk * 16 * D + (d >> 5) * 512 + t * 128 + ((g + 2 * t) & 7) * 16 + ((d >> 4) & 1) * 8;
 }
-// Codes of a quad into a region: keys of rows [from, to), values of all four rows.
-template <int D>
-__device__ __forceinline__ void put_quad(unsigned char* at, int blk, int t, int d, const Quad& q, float inv, int which, int kind, int from, int to) {
-  unsigned int c[4][4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[k][i] = code_pair(q.row[k].x[2 * i] * inv, q.row[k].x[2 * i + 1] * inv, kind);
+// Codes of a quad times inv into a region: keys of rows [from, to), values of all four rows.
+template <int D, int kKind>
+__device__ __forceinline__ void put_quad(unsigned char* at, int blk, int t, int d, const Quad& q, float inv, int which, int from, int to) {
   if (which == 0) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = quad_row(blk, t, k);
-      if (r >= from && r < to) *reinterpret_cast<uint2*>(at + key_at<D>(r, d)) = make_uint2(c[k][0] | c[k][1] << 16, c[k][2] | c[k][3] << 16);
+      const float* x = q.row[k].x;
+      const uint2 w = make_uint2(word_of<kKind>(x[0], x[1], x[2], x[3], inv), word_of<kKind>(x[4], x[5], x[6], x[7], inv));
+      if (r >= from && r < to) *reinterpret_cast<uint2*>(at + key_at<D>(r, d)) = w;
     }
   } else {
-    unsigned int w[8];                                   // a dim each
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned int x = c[0][i] | c[1][i] << 16, y = c[2][i] | c[3][i] << 16;
-      w[2 * i] = __byte_perm(x, y, 0x6420); w[2 * i + 1] = __byte_perm(x, y, 0x7531);
-    }
+    auto dim = [&](int i) { return word_of<kKind>(q.row[0].x[i], q.row[1].x[i], q.row[2].x[i], q.row[3].x[i], inv); };
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       const int i = 4 * (p >> 1) + (p & 1);
-      *reinterpret_cast<uint2*>(at + quad_values_at<D>(blk, t, d, p)) = make_uint2(w[i], w[i + 2]);
+      *reinterpret_cast<uint2*>(at + quad_values_at<D>(blk, t, d, p)) = make_uint2(dim(i), dim(i + 2));
     }
   }
 }
 // Codes of eight dims of one row; other rows' codes stay.
-template <int D>
-__device__ __forceinline__ void put_row(unsigned char* at, int r, int d, const Eight& x, float inv, int which, int kind) {
-  unsigned int c[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = code_pair(x.x[2 * i] * inv, x.x[2 * i + 1] * inv, kind);
+template <int D, int kKind>
+__device__ __forceinline__ void put_row(unsigned char* at, int r, int d, const Eight& x, float inv, int which) {
+  const unsigned int c[2] = {word_of<kKind>(x.x[0], x.x[1], x.x[2], x.x[3], inv), word_of<kKind>(x.x[4], x.x[5], x.x[6], x.x[7], inv)};
   if (which == 0) {
-    *reinterpret_cast<uint2*>(at + key_at<D>(r, d)) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    *reinterpret_cast<uint2*>(at + key_at<D>(r, d)) = make_uint2(c[0], c[1]);
   } else {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       unsigned char* w = at + quad_values_at<D>(r >> 4, (r & 7) >> 1, d, p) + (r >> 3 & 1) * 2 + (r & 1);
-      const int i = 4 * (p >> 1) + (p & 1);
-      w[0] = (unsigned char)(c[i >> 1] >> (i & 1) * 8); w[4] = (unsigned char)(c[(i + 2) >> 1] >> (i & 1) * 8);
+      w[0] = (unsigned char)(c[p >> 1] >> (p & 1) * 8); w[4] = (unsigned char)(c[p >> 1] >> ((p & 1) * 8 + 16));
     }
   }
-}
-__device__ __forceinline__ Eight eight_of(unsigned int lo, unsigned int hi, float scale, int kind) {
-  Eight e;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e.x[i] = code_value(((i < 4 ? lo : hi) >> (i & 3) * 8) & 0xFF, kind) * scale;
-  return e;
 }
 // A quad's raw words: keys of rows below `to`, values of all rows.
 struct QuadWords { uint2 v[4]; };
@@ -171,12 +180,37 @@ __device__ __forceinline__ QuadWords get_words(const unsigned char* at, int blk,
   }
   return q;
 }
-// Row k of a quad as numbers.
-__device__ __forceinline__ Eight row_of(const QuadWords& q, int k, float scale, int which, int kind) {
-  if (which == 0) return eight_of(q.v[k].x, q.v[k].y, scale, kind);
-  // word of dim i: pair 2 (i / 4) + i % 2, half (i / 2) % 2
-  auto byte = [&](int i) { const uint2 v = q.v[2 * (i >> 2) + (i & 1)]; return ((i >> 1 & 1 ? v.y : v.x) >> k * 8) & 0xFF; };
-  return eight_of(byte(0) | byte(1) << 8 | byte(2) << 16 | byte(3) << 24, byte(4) | byte(5) << 8 | byte(6) << 16 | byte(7) << 24, scale, kind);
+template <int kKind>
+__device__ __forceinline__ Eight eight_of(uint2 w, float scale) {
+  Eight e;
+  values_of<kKind>(w.x, scale, e.x);
+  values_of<kKind>(w.y, scale, e.x + 4);
+  return e;
+}
+// All four rows of a quad as numbers.
+template <int kKind>
+__device__ __forceinline__ Quad quad_of(const QuadWords& w, float scale, int which) {
+  Quad q;
+  if (which == 0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q.row[k] = eight_of<kKind>(w.v[k], scale);
+  } else {                   // a word is one dim of the four rows
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x[4];
+        values_of<kKind>(e ? w.v[p].y : w.v[p].x, scale, x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q.row[k].x[4 * (p >> 1) + (p & 1) + 2 * e] = x[k];
+      }
+  }
+  return q;
+}
+// Row k of a quad of values: its eight bytes as two words of four dims.
+__device__ __forceinline__ uint2 row_of_values(const QuadWords& w, int k) {
+  auto four = [&](uint2 a, uint2 b) { return __byte_perm(__byte_perm(a.x, b.x, k | (k + 4) << 4), __byte_perm(a.y, b.y, k | (k + 4) << 4), 0x5410); };
+  return make_uint2(four(w.v[0], w.v[1]), four(w.v[2], w.v[3]));
 }
 
 // ---- rows in ------------------------------------------------------------------------------------------------------------
@@ -195,8 +229,8 @@ struct AppendArgs {
 };
 
 // Turns eight dims d.. of a row; cs(i) gives (A cos, A sin) of pair i.
-template <typename F>
-__device__ __forceinline__ void turn_row(Eight& x, const AppendArgs& a, const unsigned short* line, int d, int io, F cs) {
+template <int kIo, typename F>
+__device__ __forceinline__ void turn_row(Eight& x, const AppendArgs& a, const unsigned short* line, int d, F cs) {
   if (d >= a.rot) return;
   const int half = a.rot / 2;
   if (a.pairs) {
@@ -209,12 +243,12 @@ __device__ __forceinline__ void turn_row(Eight& x, const AppendArgs& a, const un
       }
   } else {
     Eight y;
-    if (a.vec) y = unpack8(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)), io);
+    if (a.vec) y = unpack8<kIo>(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)));
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (d + e < a.rot) {
         const bool lower = d + e < half;
-        if (!a.vec) y.x[e] = load16(line[lower ? d + e + half : d + e - half], io);
+        if (!a.vec) y.x[e] = load16<kIo>(line[lower ? d + e + half : d + e - half]);
         const float2 f = cs(lower ? d + e : d + e - half);
         x.x[e] = lower ? x.x[e] * f.x - y.x[e] * f.y : y.x[e] * f.y + x.x[e] * f.x;
       }
@@ -225,18 +259,41 @@ __device__ __forceinline__ float2 turned_by(const AppendArgs& a, int pos, int pa
   turn_of(pos, a.turns[pair], c, s);
   return make_float2(a.amplitude * c, a.amplitude * s);
 }
-__device__ __forceinline__ void largest(const Eight& x, float& most, bool& odd) {
+// The largest magnitude of eight raw numbers so far, as bits of their type, two at a time: magnitudes order like integers, and
+// infinities and NaN are above all numbers.
+__device__ __forceinline__ unsigned int largest_bits(unsigned int most, uint4 v) {
+  return __vmaxu2(__vmaxu2(most, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu)), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+}
+template <int kIo>
+__device__ __forceinline__ bool has_odd(unsigned int bits) {       // an infinity or NaN among them
+  constexpr unsigned int inf = kIo == DKV_BF16 ? 0x7F80u : 0x7C00u;
+  return (bits & 0xFFFF) >= inf || bits >> 16 >= inf;
+}
+template <int kIo>
+__device__ __forceinline__ float largest_of(unsigned int bits) { return load16<kIo>((unsigned short)max(bits & 0xFFFF, bits >> 16)); }
+// The largest finite magnitude of eight numbers; NaN becomes 0 and what is infinite the largest float.  Whether there were some.
+__device__ __forceinline__ bool settle(Eight& x, float& most) {
+  bool odd = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float m = fabsf(x.x[e]);
-    if (m < INFINITY) most = fmaxf(most, m); else odd = true;
+    if (m < INFINITY) most = fmaxf(most, m);
+    else { odd = true; x.x[e] = m == INFINITY ? copysignf(3.402823466e38f, x.x[e]) : 0.f; }
   }
+  return odd;
+}
+// Numbers that settle() changed, cut to the largest code once the scale is known.
+template <int kKind>
+__device__ __forceinline__ void cut(Eight& x, float scale) {
+  const float most = (kKind == kE4m3 ? 448.f : 127.f) * scale;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x.x[e] = fminf(fmaxf(x.x[e], -most), most);
 }
 // Whether `add` rows go behind the `len` rows of a sequence; if not, why (a status bit), else 0.
 __device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, const int* table, int len, int held, int add) {
   if (add < 0 || add > a.cap) return kBadArgument;
-  if ((long long)len + add > (long long)held * c.R) return kNoRoom;
-  return add > 0 && len % c.R && c.refs[table[len / c.R]] != 1 ? kNoRoom : 0;
+  if ((long long)len + add > (long long)held << c.shift) return kNoRoom;
+  return add > 0 && len & (c.R - 1) && c.refs[table[len >> c.shift]] != 1 ? kNoRoom : 0;
 }
 
 // Many rows: the new rows of one page, `per` heads and tensors one after the other.  Their largest magnitude gives the scale; where
@@ -245,13 +302,13 @@ __device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, con
 // bytes in, 1 out), but for the chain of loads at a block's start and the ticket at its end, which is why a block has several heads
 // where there are blocks enough.  Angles are shared by all heads (shared memory, [R][rot/2]).  grid (pages a sequence can touch,
 // 2 Hkv / per, n); the last block of a sequence to arrive (a ticket) makes the rows part of it.
-template <int D, int R>
-__global__ void __launch_bounds__(R * D / 32)
+constexpr int kQuadThreads = 512;                                            // R * D / 32 threads, at most
+template <int D, int kKind, int kIo>
+__global__ void __launch_bounds__(kQuadThreads)
 append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
-  constexpr int kThreads = R * D / 32;
   extern __shared__ float2 turn_s[];
-  __shared__ float warp_s[2][kThreads / 32];
-  const int tid = threadIdx.x, i = blockIdx.z, seq = a.first + i * a.step;
+  __shared__ float warp_s[2][kQuadThreads / 32];
+  const int R = c.R, tid = threadIdx.x, i = blockIdx.z, seq = a.first + i * a.step;
   const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   pdl_launch();
   pdl_wait();
@@ -262,7 +319,7 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
     if (not_ok && tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) report(c, not_ok, seq);
     return;
   }
-  const int slot = len / R + blockIdx.x, base = slot * R;
+  const int slot = (len >> c.shift) + blockIdx.x, base = slot << c.shift;
   const int r0 = max(0, len - base), r1 = min(R, len + add - base);          // the page's new rows
   if (r0 < r1) {
     const int page = table[slot], y0 = blockIdx.y * a.per, y1 = min(2 * c.Hkv, y0 + a.per);
@@ -281,7 +338,7 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
     Raw raw = ask(y0);
     if (a.rot) {
       const int pos0 = a.pos0[i] + base - len;
-      for (int x = tid; x < (r1 - r0) * (a.rot / 2); x += kThreads) {
+      for (int x = tid; x < (r1 - r0) * (a.rot / 2); x += blockDim.x) {
         const int r = r0 + x / (a.rot / 2), pair = x % (a.rot / 2);
         turn_s[r * (a.rot / 2) + pair] = turned_by(a, pos0 + r, pair);
       }
@@ -293,26 +350,37 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
       unsigned char* to = c.pages + reg * (size_t)(R * D);
       const Raw now = raw;
       if (y + 1 < y1) raw = ask(y + 1);
+      const bool turned = a.rot && !which;
       Quad x;
-      float most = 0.f;
-      bool odd = false;
+      unsigned int bits = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        x.row[k] = unpack8(now.v[k], c.io);
-        if (a.rot && !which && is_new(k)) turn_row(x.row[k], a, line(y, k), d, c.io, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
-        largest(x.row[k], most, odd);
+        bits = largest_bits(bits, now.v[k]);
+        x.row[k] = unpack8<kIo>(now.v[k]);
+        if (turned && is_new(k)) turn_row<kIo>(x.row[k], a, line(y, k), d, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
       }
-      if (odd) report(c, kNotFinite, seq);
-      int e = scale_exponent(block_max(most, warp_s[y & 1]), c.kind);
+      float most = largest_of<kIo>(bits);
+      bool odd = has_odd<kIo>(bits);
+      if (turned || odd) {                                                   // the numbers themselves: turned, or not all of them finite
+        most = 0.f;
+        odd = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) odd |= settle(x.row[k], most);
+        if (odd) report(c, kNotFinite, seq);
+      }
+      int e = scale_exponent(block_max(most, warp_s[y & 1]), kKind);
       if (r0) {
         const float old = c.scales[reg];
         e = max(e, exponent_of(old));
-        const QuadWords w = get_words<D>(to, blk, t, d, which, r0);
+        const Quad w = quad_of<kKind>(get_words<D>(to, blk, t, d, which, r0), old, which);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (quad_row(blk, t, k) < r0) x.row[k] = row_of(w, k, old, which, c.kind);
+        for (int k = 0; k < 4; ++k) if (quad_row(blk, t, k) < r0) x.row[k] = w.row[k];
         __syncthreads();                                                     // the whole block has read the old scale
       }
-      put_quad<D>(to, blk, t, d, x, pow2(-e), which, c.kind, 0, r1);
+      if (odd)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) cut<kKind>(x.row[k], pow2(e));
+      put_quad<D, kKind>(to, blk, t, d, x, pow2(-e), which, 0, r1);
       if (tid == 0) c.scales[reg] = pow2(e);
     }
   }
@@ -330,9 +398,10 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
 // Latency: the new rows are on their way while the sequence's length, its table and the page's scale are looked up one after the
 // other; then every lane writes its eight codes of a row.  Only where the scale of a page with rows grows is the page read.  grid (n).
 constexpr int kFewRows = 8, kFewWarps = 16;
-template <int D, int R>
+template <int D, int kKind, int kIo>
 __global__ void __launch_bounds__(kFewWarps * 32)
 append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
+  const int R = c.R;
   constexpr int kPer = kFewRows * D / 256;                                   // pieces (a row, eight dims) of a lane
   const int lane = threadIdx.x & 31, i = blockIdx.x, seq = a.first + i * a.step;
   pdl_launch();
@@ -361,12 +430,12 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
 #pragma unroll
     for (int p = 0; p < kPer; ++p) {
       const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8;
-      x[p] = unpack8(raw[p], c.io);
-      if (a.rot && !which && j < add) turn_row(x[p], a, from + j * src.token, d, c.io, [&](int pair) { return turned_by(a, pos0 + j, pair); });
+      x[p] = unpack8<kIo>(raw[p]);
+      if (a.rot && !which && j < add) turn_row<kIo>(x[p], a, from + j * src.token, d, [&](int pair) { return turned_by(a, pos0 + j, pair); });
     }
-    for (int base = len / R * R; base < len + add; base += R) {
+    for (int base = len & -R; base < len + add; base += R) {
       const int r0 = max(0, len - base), r1 = min(R, len + add - base);
-      const size_t reg = region(c, table[base / R], h, which);
+      const size_t reg = region(c, table[base >> c.shift], h, which);
       unsigned char* to = c.pages + reg * (size_t)(R * D);
       const float old = c.scales[reg];
       float most = 0.f;
@@ -374,21 +443,17 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
 #pragma unroll
       for (int p = 0; p < kPer; ++p) {
         const int j = (lane + 32 * p) / (D / 8), r = len + j - base;
-        if (j < add && r >= r0 && r < r1) largest(x[p], most, odd);
+        if (j < add && r >= r0 && r < r1) odd |= settle(x[p], most);
       }
       if (odd) report(c, kNotFinite, seq);
 #pragma unroll
       for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-      int e = scale_exponent(most, c.kind);
+      int e = scale_exponent(most, kKind);
       if (r0 && e > exponent_of(old)) {                                      // the page's older codes are rounded again
         for (int u = lane; u < R * D / 32; u += 32) {
           const int d = u % (D / 8) * 8, t = u / (D / 8) % 4, blk = u / (D / 2);
           if (quad_row(blk, t, 0) >= r0) continue;                           // (row 0 is a quad's lowest)
-          const QuadWords w = get_words<D>(to, blk, t, d, which, r0);
-          Quad q;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) q.row[k] = row_of(w, k, old, which, c.kind);
-          put_quad<D>(to, blk, t, d, q, pow2(-e), which, c.kind, 0, r0);
+          put_quad<D, kKind>(to, blk, t, d, quad_of<kKind>(get_words<D>(to, blk, t, d, which, r0), old, which), pow2(-e), which, 0, r0);
         }
         __syncwarp();                                                        // the new rows share words with the old ones
       } else if (r0) {
@@ -398,7 +463,10 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
 #pragma unroll
       for (int p = 0; p < kPer; ++p) {
         const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8, r = len + j - base;
-        if (j < add && r >= r0 && r < r1) put_row<D>(to, r, d, x[p], inv, which, c.kind);
+        if (j < add && r >= r0 && r < r1) {
+          cut<kKind>(x[p], pow2(e));
+          put_row<D, kKind>(to, r, d, x[p], inv, which);
+        }
       }
       __syncwarp();                                                          // every lane has read the old scale
       if (lane == 0 && (!r0 || e != exponent_of(old))) c.scales[reg] = pow2(e);
@@ -414,10 +482,10 @@ struct ReadArgs { Rows8 k, v; int first, step, cap; };
 
 // The rows of one page, head and tensor as 16-bit numbers, a quad a thread; rows past the sequence's length are not written.
 // Bound by HBM.  grid (pages of `cap` rows, 2 Hkv, n).
-template <int D, int R>
-__global__ void __launch_bounds__(R * D / 32)
+template <int D, int kKind, int kIo>
+__global__ void __launch_bounds__(kQuadThreads)
 read8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ ReadArgs a) {
-  const int tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
+  const int R = c.R, tid = threadIdx.x, h = blockIdx.y >> 1, which = blockIdx.y & 1, i = blockIdx.z, seq = a.first + i * a.step;
   const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   pdl_launch();
   pdl_wait();
@@ -428,15 +496,11 @@ read8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ ReadArgs 
   const float scale = c.scales[reg];
   const Rows8& dst = which ? a.v : a.k;
   unsigned short* to = static_cast<unsigned short*>(const_cast<void*>(dst.data)) + i * dst.batch + h * dst.head + d;
+  const Quad q = quad_of<kKind>(w, scale, which);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int r = quad_row(blk, t, k);
-    if (r >= rows) continue;
-    const Eight e = row_of(w, k, scale, which, c.kind);
-    unsigned int o[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) o[q] = store16(e.x[2 * q], c.io) | store16(e.x[2 * q + 1], c.io) << 16;
-    *reinterpret_cast<uint4*>(to + (base + r) * dst.token) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (r < rows) *reinterpret_cast<uint4*>(to + (base + r) * dst.token) = pack8<kIo>(q.row[k]);
   }
 }
 
@@ -654,11 +718,11 @@ struct CompactArgs {
 // One page and head of a compacted sequence: row j is row idx[j] of the sequence as it is; a new page takes the scales that its rows
 // need.  A quad of keys and one of values a thread, all their loads in flight.  A row's values lie in 32 bytes of every 128, so four
 // times their bytes are read.  grid (pages of `cols` rows, Hkv, n).
-template <int D, int R>
-__global__ void __launch_bounds__(R * D / 32)
+template <int D, int kKind>
+__global__ void __launch_bounds__(kQuadThreads)
 compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ CompactArgs a) {
-  __shared__ float warp_s[2][R * D / 1024];
-  const int tid = threadIdx.x, h = blockIdx.y, i = blockIdx.z, seq = a.first + i * a.step;
+  __shared__ float warp_s[2][kQuadThreads / 32];
+  const int R = c.R, tid = threadIdx.x, h = blockIdx.y, i = blockIdx.z, seq = a.first + i * a.step;
   const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   const int* idx = a.idx + ((size_t)i * c.Hkv + h) * a.cols + blockIdx.x * R;
   pdl_launch();
@@ -676,7 +740,7 @@ compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Compac
     const bool wanted = quad_row(blk, t, k) < rows, inside = wanted && from[k] >= 0 && from[k] < len;
     if (wanted && !inside) report(c, kBadArgument, seq);
     if (!inside) from[k] = -1;
-    reg[k] = inside ? region(c, table[from[k] / R], h, 0) : 0;
+    reg[k] = inside ? region(c, table[from[k] >> c.shift], h, 0) : 0;
   }
   uint2 key[4];
   QuadWords value[4];
@@ -685,7 +749,7 @@ compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Compac
   for (int k = 0; k < 4; ++k)
     if (from[k] >= 0) {
       const unsigned char* at = c.pages + reg[k] * (size_t)(R * D);
-      const int r = from[k] % R;
+      const int r = from[k] & (R - 1);
       key[k] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
       value[k] = get_words<D>(at + R * D, r >> 4, (r & 7) >> 1, d, 1, R);
       scale[k] = *reinterpret_cast<const float2*>(c.scales + reg[k]);
@@ -697,19 +761,17 @@ compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Compac
     float most = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (from[k] < 0) {
+      if (from[k] >= 0) {
+        x.row[k] = eight_of<kKind>(which ? row_of_values(value[k], (from[k] & 1) + 2 * (from[k] >> 3 & 1)) : key[k], which ? scale[k].y : scale[k].x);
+      } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
-      } else if (which == 0) {
-        x.row[k] = eight_of(key[k].x, key[k].y, scale[k].x, c.kind);
-      } else {
-        x.row[k] = row_of(value[k], (from[k] & 1) + 2 * (from[k] >> 3 & 1), scale[k].y, 1, c.kind);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
     }
-    const int e = scale_exponent(block_max(most, warp_s[which]), c.kind);
-    put_quad<D>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(-e), which, c.kind, 0, rows);
+    const int e = scale_exponent(block_max(most, warp_s[which]), kKind);
+    put_quad<D, kKind>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(-e), which, 0, rows);
     if (tid == 0) c.scales[to + which] = pow2(e);
   }
 }
