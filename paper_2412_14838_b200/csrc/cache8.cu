@@ -349,6 +349,7 @@ int dkv_cache8_append(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   // Heads and tensors a block: as many as leave four blocks an SM.
   const long long blocks = 2ll * c->cfg.n_kv_heads * pages * n;
   a.per = (int)std::min<long long>(2 * c->cfg.n_kv_heads, std::max(1ll, blocks / (4 * c->n_sms)));
+  a.per = 2 * c->cfg.n_kv_heads / ((2 * c->cfg.n_kv_heads + a.per - 1) / a.per);
   C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto io) {
     constexpr int D = decltype(d)::value, K = decltype(kind)::value, I = decltype(io)::value;
     if (k->tokens <= kFewRows) return launch_pdl(append8_few_kernel<D, K, I>, dim3(n), std::min(2 * c->cfg.n_kv_heads, kFewWarps) * 32, 0, 1, as_stream(stream), c->view, a);
