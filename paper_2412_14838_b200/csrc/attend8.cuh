@@ -41,7 +41,7 @@ __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // (a, b) += (x, y) * f, as one packed instruction.
-__device__ __forceinline__ void fma2(float& a, float& b, float x, float y, float f) {
+__device__ __forceinline__ void add_scaled2(float& a, float& b, float x, float y, float f) {
   asm("{.reg .b64 p, q, r; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mov.b64 r, {%4, %4}; fma.rn.f32x2 p, q, r, p; mov.b64 {%0, %1}, p;}" : "+f"(a), "+f"(b) : "f"(x), "f"(y), "f"(f));
 }
 // Four codes as two pairs of fp16.
@@ -228,7 +228,7 @@ struct AttendWarp {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int x = 0; x < 4; x += 2) fma2(acc[4 * p + e][x], acc[4 * p + e][x + 1], o[e][x], o[e][x + 1], vs);
+        for (int x = 0; x < 4; x += 2) add_scaled2(acc[4 * p + e][x], acc[4 * p + e][x + 1], o[e][x], o[e][x + 1], vs);
     }
   }
 

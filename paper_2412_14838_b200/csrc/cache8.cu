@@ -7,6 +7,7 @@
 #include <stdlib.h>
 #include <string.h>
 #include <algorithm>
+#include <atomic>
 #include <new>
 #include <type_traits>
 #include <vector>
@@ -72,21 +73,31 @@ bool valid(const dkv_rotary* r) {
 
 // ---- rotary positions ---------------------------------------------------------------------------------------------------
 template <typename T, int V>
-cudaError_t launch_rotate(RotateArgs& a, int head_dim, cudaStream_t st) {
+cudaError_t launch_rotate(RotateArgs& a, int head_dim, bool pairs, int sms, cudaStream_t st) {
   a.rot_pieces = a.rot / (2 * V);
   a.pieces = head_dim / (2 * V);
-  a.threads *= a.pieces;                       // so far the tokens
-  const long long blocks = (a.threads + kRotateThreads - 1) / kRotateThreads;
+  // As many tokens a block as leave two blocks an SM, few heads' cosines being shared otherwise; the rest of its threads deal out heads.
+  a.block_tokens = (int)std::max(1ll, std::min<long long>(std::min(kRotateTokens, kRotateThreads / a.pieces), a.all / (2 * sms)));
+  a.groups = std::max(1, std::min(a.heads, kRotateThreads / (a.pieces * a.block_tokens)));
+  const long long blocks = (a.all + a.block_tokens - 1) / a.block_tokens;
   if (blocks > INT_MAX) return cudaErrorInvalidValue;
-  // Heads a thread: few while there are not enough threads to fill the GPU, more to use its cosines again.
-  int per = 1;
-  while (per < 16 && per < a.heads && blocks * ((a.heads + 2 * per - 1) / (2 * per)) >= 148 * 8) per *= 2;
-  a.heads_a_thread = per;
-  return launch_pdl(rotate_kernel<T, V>, dim3((unsigned)blocks, (a.heads + per - 1) / per), kRotateThreads, 0, 1, st, a);
+  const int splits = (int)std::max(1ll, std::min<long long>((a.heads + a.groups - 1) / a.groups, sms / blocks));      // blocks that share a token's heads
+  const size_t smem = (size_t)a.block_tokens * ((a.rot / 2 + 1) / 2 * 2 + 2) * sizeof(float2);
+  return launch_pdl(pairs ? rotate_kernel<T, V, true> : rotate_kernel<T, V, false>, dim3((unsigned)blocks, splits), kRotateThreads, smem, 1, st, a);
 }
 template <typename T>
-cudaError_t launch_rotate(RotateArgs& a, int head_dim, bool wide, cudaStream_t st) {
-  return wide ? launch_rotate<T, 16 / (int)sizeof(T)>(a, head_dim, st) : launch_rotate<T, 1>(a, head_dim, st);
+cudaError_t launch_rotate(RotateArgs& a, int head_dim, bool wide, bool pairs, int sms, cudaStream_t st) {
+  return wide ? launch_rotate<T, 16 / (int)sizeof(T)>(a, head_dim, pairs, sms, st) : launch_rotate<T, 1>(a, head_dim, pairs, sms, st);
+}
+// Of the current device, asked for once a device: a launch's shape depends on it, its result does not.
+int sm_count() {
+  static std::atomic<int> known[64];
+  int device = 0, n = 148;
+  if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return n;
+  if ((n = known[device].load(std::memory_order_relaxed)) > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 148;
+  known[device].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 // ---- the cache ----------------------------------------------------------------------------------------------------------
@@ -238,13 +249,15 @@ int dkv_rotate(const dkv_rotary* r, const int32_t* pos, const dkv_rows* x, const
   const int per = 16 / element_size(x->type);
   wide = wide && r->rot_dim % (2 * per) == 0 && (r->head_dim - r->rot_dim) % (2 * per) == 0;
   a.pos = pos;
-  a.threads = (long long)x->batch * x->tokens; a.tokens = x->tokens;
-  a.rot = r->rot_dim; a.pairs = r->layout == DKV_ROTARY_PAIRS; a.in_place = in_place;
+  a.all = (long long)x->batch * x->tokens; a.tokens = x->tokens;
+  a.rot = r->rot_dim; a.in_place = in_place;
+  const bool pairs = r->layout == DKV_ROTARY_PAIRS;
+  const int sms = sm_count(), D = r->head_dim;
   a.amplitude = r->amplitude; a.sign = transpose ? -1.f : 1.f;
   memcpy(a.turns, r->turns, sizeof a.turns);
   cudaStream_t st = as_stream(stream);
-  const cudaError_t e = x->type == DKV_F32 ? launch_rotate<float>(a, r->head_dim, wide, st) : x->type == DKV_F16 ? launch_rotate<__half>(a, r->head_dim, wide, st)
-                                                                                          : launch_rotate<__nv_bfloat16>(a, r->head_dim, wide, st);
+  const cudaError_t e = x->type == DKV_F32 ? launch_rotate<float>(a, D, wide, pairs, sms, st) : x->type == DKV_F16 ? launch_rotate<__half>(a, D, wide, pairs, sms, st)
+                                                                                                : launch_rotate<__nv_bfloat16>(a, D, wide, pairs, sms, st);
   return e == cudaSuccess ? DKV_OK : fail(nullptr, e);
 }
 
