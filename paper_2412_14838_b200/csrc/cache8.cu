@@ -24,7 +24,7 @@ struct dkv_cache8 {
   dkv_cache8_config cfg;
   int device, n_sms;
   Cache8 view;
-  int *d_prefix, *d_pick, *d_jobs, *d_new_table, *d_new_held;     // scratch of the calls on pages
+  int *d_pick, *d_jobs, *d_new_table, *d_new_held;     // scratch of the calls on pages
   unsigned int* d_tickets;      // [n_seqs * Hkv], zero between launches
   float* d_scratch;             // parts of heads that lie in several blocks' slices
   long long launches;
@@ -114,7 +114,7 @@ int validate(const dkv_cache8_config* c) {
 
 int free_cache(dkv_cache8* c) {
   for (void* p : {(void*)c->view.pages, (void*)c->view.scales, (void*)c->view.table, (void*)c->view.len, (void*)c->view.held, (void*)c->view.refs,
-                  (void*)c->view.free, (void*)c->view.hint, (void*)c->view.status, (void*)c->d_prefix, (void*)c->d_pick, (void*)c->d_jobs,
+                  (void*)c->view.free, (void*)c->view.hint, (void*)c->view.status, (void*)c->d_pick, (void*)c->d_jobs,
                   (void*)c->d_new_table, (void*)c->d_new_held, (void*)c->d_tickets, (void*)c->d_scratch})
     cudaFree(p);
   delete c;
@@ -287,7 +287,6 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   TRY(cudaMalloc(&v.free, sizeof(int) * words));
   TRY(cudaMalloc(&v.hint, sizeof(int)));
   TRY(cudaMalloc(&v.status, sizeof(int) * 2));
-  TRY(cudaMalloc(&c->d_prefix, sizeof(int) * (cfg->n_seqs + 1)));
   TRY(cudaMalloc(&c->d_pick, sizeof(int) * cfg->n_pages));
   TRY(cudaMalloc(&c->d_jobs, sizeof(int) * (1 + 2 * cfg->n_seqs)));
   TRY(cudaMalloc(&c->d_new_table, entries * sizeof(int)));
@@ -339,7 +338,7 @@ int dkv_cache8_reserve(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   if (int rc = check(c, first, n, step)) return rc;
   if (!aligned(rows, 4) || (!rows && add < 0)) return DKV_ERR_INVALID_ARG;
   if (n == 0) return DKV_OK;
-  PlanArgs a = {rows, c->d_prefix, c->d_pick, c->d_jobs, nullptr, nullptr, first, step, n, add};
+  PlanArgs a = {rows, c->d_pick, c->d_jobs, nullptr, nullptr, first, step, n, add};
   C8_LAUNCH(c, launch_pdl(reserve8_kernel, dim3(kPlanBlocks), kPlanThreads, 0, kPlanBlocks, as_stream(stream), c->view, a));
   return DKV_OK;
 }
@@ -429,7 +428,7 @@ int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   if (int rc = check(c, first, n, step)) return rc;
   if (heads != c->cfg.n_kv_heads || cols < 0 || (cols && !idx) || !aligned(idx, 4) || !aligned(count, 4)) return DKV_ERR_INVALID_ARG;
   if (n == 0) return DKV_OK;
-  const PlanArgs p = {count, c->d_prefix, c->d_pick, c->d_jobs, c->d_new_table, c->d_new_held, first, step, n, cols};
+  const PlanArgs p = {count, c->d_pick, c->d_jobs, c->d_new_table, c->d_new_held, first, step, n, cols};
   const CompactArgs a = {idx, count, c->d_new_table, c->d_new_held, first, step, cols};
   cudaStream_t st = as_stream(stream);
   C8_LAUNCH(c, launch_pdl(plan_compact8_kernel, dim3(1), kPlanThreads, 0, 1, st, c->view, p));

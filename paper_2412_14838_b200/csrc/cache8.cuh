@@ -510,7 +510,6 @@ constexpr int kPlanThreads = 1024;
 
 struct PlanArgs {
   const int* count;          // [n] or null: `most` each
-  int* prefix;               // [n + 1] scratch: pages that sequences before i need
   int* pick;                 // [n_pages] scratch: the pages found
   int* jobs;                 // [1 + 2 n] scratch: how many pages have to be copied, (from, to) of each
   int* new_table;            // [sequence][max_pages], compaction: the pages to be
@@ -546,93 +545,92 @@ __device__ __forceinline__ long long block_scan(long long v, long long* warp_s, 
 template <bool kCompact>
 __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
   __shared__ long long warp_s[32];
-  __shared__ int jobs_s;
+  __shared__ int jobs_s, prefix_s[kPlanThreads + 1], len_s[kPlanThreads], held_s[kPlanThreads], copies_s[kPlanThreads];
   const int tid = threadIdx.x;
   if (tid == 0) jobs_s = 0;
-  auto own_copy = [&](int seq, int len) { return len % c.R && c.refs[c.table[(size_t)seq * c.max_pages + len / c.R]] > 1; };
-  int all = 0;
+  // Sequences that are served get the pages given out one call after the other, kPlanThreads sequences at a time, as if in one.
+  bool lasts = true;
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
-    const int i = i0 + tid, seq = a.first + i * a.step;
-    int need = 0;
+    const int i = i0 + tid, n = min(kPlanThreads, a.n - i0), seq = a.first + i * a.step;
+    int need = 0, pages = 0;
     if (i < a.n) {
       const int count = a.count ? a.count[i] : a.most;
       if (kCompact) {
-        const bool bad = count < 0 || count > a.most;
-        if (bad) report(c, kBadArgument, seq);
-        need = bad ? 0 : (int)(((long long)count + c.R - 1) / c.R);
-        if (need > c.max_pages) { report(c, kTableFull, seq); need = 0; a.new_held[seq] = -1; }
-        else a.new_held[seq] = bad ? -1 : need;
+        pages = need = (int)(((long long)count + c.R - 1) >> c.shift);
+        const bool bad = count < 0 || count > a.most, full = !bad && need > c.max_pages;
+        if (bad || full) { report(c, bad ? kBadArgument : kTableFull, seq); need = 0; }
+        a.new_held[seq] = bad || full ? -1 : need;
       } else {
         const int len = c.len[seq], held = c.held[seq];
-        const long long pages = ((long long)len + count + c.R - 1) / c.R;
+        const long long all = ((long long)len + count + c.R - 1) >> c.shift;
+        bool copies = false;
         if (count < 0) report(c, kBadArgument, seq);
-        else if (pages > c.max_pages) report(c, kTableFull, seq);
-        else if (count > 0) need = max(0, (int)pages - held) + own_copy(seq, len);
+        else if (all > c.max_pages) report(c, kTableFull, seq);
+        else if (count > 0) {
+          copies = len & (c.R - 1) && __ldcg(c.refs + __ldcg(c.table + (size_t)seq * c.max_pages + (len >> c.shift))) > 1;
+          need = max(0, (int)all - held) + copies;
+          pages = max(held, (int)all);
+        }
+        len_s[tid] = len; held_s[tid] = held; copies_s[tid] = copies;
       }
     }
-    long long total;                                                         // sums stop at n_pages + 1: more than there can be
-    const long long before = block_scan(need, warp_s, total);
-    if (i < a.n) a.prefix[i] = (int)min(all + before, c.n_pages + 1ll);
-    all = (int)min(all + total, c.n_pages + 1ll);
-  }
-  if (tid == 0) { a.prefix[a.n] = all; if (!kCompact) a.jobs[0] = 0; }
-  if (all == 0) return;
-  // the lowest `all` free pages
-  const int words = (c.n_pages + 31) / 32;
-  int found = 0;
-  for (int w0 = *c.hint; w0 < words && found < all; w0 += kPlanThreads) {
-    const int w = w0 + tid;
-    unsigned int bits = w < words ? c.free[w] : 0;
-    long long total;
-    int at = found + (int)block_scan(__popc(bits), warp_s, total);
-    for (; bits && at < all; bits &= bits - 1) {
-      if (at < c.n_pages) a.pick[at] = w * 32 + __ffs(bits) - 1;
-      ++at;
-    }
-    found += (int)total;
-  }
-  __syncthreads();
-  found = min(found, all);
-  if (tid == 0 && found == all) *c.hint = a.pick[all - 1] >> 5;
-  __syncthreads();
-  for (int k = tid; k < found; k += kPlanThreads) {
-    int lo = 0, hi = a.n - 1;                                                // the last sequence with prefix <= k
-    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (a.prefix[mid] <= k) lo = mid; else hi = mid - 1; }
-    if (a.prefix[lo + 1] > found) continue;                                  // not served
-    const int seq = a.first + lo * a.step, page = a.pick[k];
-    int j = k - a.prefix[lo];
-    if (kCompact) {
-      a.new_table[(size_t)seq * c.max_pages + j] = page;
-    } else {
-      const int len = c.len[seq], held = c.held[seq];
-      int* table = c.table + (size_t)seq * c.max_pages;
-      // whether the sequence has its last page copied follows from how many pages it got: `refs` may have changed by now
-      const int count = a.count ? a.count[lo] : a.most;
-      const int grow = max(0, (int)(((long long)len + count + c.R - 1) / c.R) - held);
-      const bool copies = a.prefix[lo + 1] - a.prefix[lo] > grow;
-      if (copies && j == 0) {
-        const int old = table[len / c.R], job = atomicAdd(&jobs_s, 1);
-        a.jobs[1 + 2 * job] = old; a.jobs[2 + 2 * job] = page;
-        table[len / c.R] = page;
-        if (atomicSub(&c.refs[old], 1) == 1) { atomicOr(&c.free[old >> 5], 1u << (old & 31)); atomicMin(c.hint, old >> 5); }
+    long long sum;                                                           // sums stop at n_pages + 1: more than there can be
+    const long long before = block_scan(need, warp_s, sum);
+    if (i < a.n) prefix_s[tid] = (int)min(before, c.n_pages + 1ll);
+    const int all = (int)min(sum, c.n_pages + 1ll);
+    if (tid == 0) prefix_s[n] = all;
+    // the lowest `all` free pages
+    const int words = (c.n_pages + 31) / 32;
+    int found = 0;
+    if (all && lasts)
+      for (int w0 = __ldcg(c.hint); w0 < words && found < all; w0 += kPlanThreads) {
+        const int w = w0 + tid;
+        unsigned int bits = w < words ? __ldcg(c.free + w) : 0;
+        long long here;
+        int at = found + (int)block_scan(__popc(bits), warp_s, here);
+        for (; bits && at < all; bits &= bits - 1) {
+          if (at < c.n_pages) a.pick[at] = w * 32 + __ffs(bits) - 1;
+          ++at;
+        }
+        found += (int)here;
+      }
+    __syncthreads();
+    found = min(found, all);
+    if (tid == 0 && all && found == all) *c.hint = a.pick[all - 1] >> 5;
+    __syncthreads();
+    for (int k = tid; k < found; k += kPlanThreads) {
+      int lo = 0, hi = n - 1;                                                // the last sequence with prefix <= k
+      while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (prefix_s[mid] <= k) lo = mid; else hi = mid - 1; }
+      if (prefix_s[lo + 1] > found) continue;                                // not served
+      const int s = a.first + (i0 + lo) * a.step, page = a.pick[k], j = k - prefix_s[lo];
+      if (kCompact) {
+        a.new_table[(size_t)s * c.max_pages + j] = page;
       } else {
-        table[held + j - copies] = page;
+        int* table = c.table + (size_t)s * c.max_pages;
+        if (copies_s[lo] && j == 0) {
+          const int at = len_s[lo] >> c.shift, old = table[at], job = atomicAdd(&jobs_s, 1);
+          a.jobs[1 + 2 * job] = old; a.jobs[2 + 2 * job] = page;
+          table[at] = page;
+          if (atomicSub(&c.refs[old], 1) == 1) { atomicOr(&c.free[old >> 5], 1u << (old & 31)); atomicMin(c.hint, old >> 5); }
+        } else {
+          table[held_s[lo] + j - copies_s[lo]] = page;
+        }
+      }
+      c.refs[page] = 1;
+      atomicAnd(&c.free[page >> 5], ~(1u << (page & 31)));
+    }
+    __syncthreads();
+    if (need) {
+      if (prefix_s[tid + 1] > found) {
+        report(c, kNoPages, seq);
+        if (kCompact) a.new_held[seq] = -1;
+      } else if (!kCompact) {
+        c.held[seq] = pages;
       }
     }
-    c.refs[page] = 1;
-    atomicAnd(&c.free[page >> 5], ~(1u << (page & 31)));
-  }
-  __syncthreads();
-  for (int i = tid; i < a.n; i += kPlanThreads) {
-    const int seq = a.first + i * a.step, need = a.prefix[i + 1] - a.prefix[i];
-    if (need == 0) continue;
-    if (a.prefix[i + 1] > found) {
-      report(c, kNoPages, seq);
-      if (kCompact) a.new_held[seq] = -1;
-    } else if (!kCompact) {
-      const int count = a.count ? a.count[i] : a.most;
-      c.held[seq] = max(c.held[seq], (int)(((long long)c.len[seq] + count + c.R - 1) / c.R));
-    }
+    lasts = lasts && found == all;
+    __threadfence();                                                         // the next sequences find `free`, `refs` and the table as they are now
+    __syncthreads();
   }
   if (!kCompact && tid == 0) a.jobs[0] = jobs_s;
 }
