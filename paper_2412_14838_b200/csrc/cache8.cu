@@ -315,7 +315,7 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   TRY(cudaStreamSynchronize(cudaStreamLegacy));
   TRY(cfg->head_dim == 64 ? set_attend_smem<64>(cfg->kind) : set_attend_smem<128>(cfg->kind));
   TRY(with_types(c, [](auto d, auto kind, auto io) {       // angles of a page's rows: the most that any cache has
-    return cudaFuncSetAttribute(append8_kernel<decltype(d)::value, decltype(kind)::value, decltype(io)::value>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(append8_kernel<decltype(d)::value, decltype(kind)::value, decltype(io)::value, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 128 * decltype(d)::value / 2 * (int)sizeof(float2));
   }));
 #undef TRY
@@ -365,7 +365,7 @@ int dkv_cache8_append(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto io) {
     constexpr int D = decltype(d)::value, K = decltype(kind)::value, I = decltype(io)::value;
     if (k->tokens <= kFewRows) return launch_pdl(append8_few_kernel<D, K, I>, dim3(n), std::min(2 * c->cfg.n_kv_heads, kFewWarps) * 32, 0, 1, as_stream(stream), c->view, a);
-    return launch_pdl(append8_kernel<D, K, I>, dim3(pages, (2 * c->cfg.n_kv_heads + a.per - 1) / a.per, n), quad_threads(c), (size_t)R * a.rot / 2 * sizeof(float2), 1,
+    return launch_pdl(rotary ? append8_kernel<D, K, I, true> : append8_kernel<D, K, I, false>, dim3(pages, (2 * c->cfg.n_kv_heads + a.per - 1) / a.per, n), quad_threads(c), (size_t)R * a.rot / 2 * sizeof(float2), 1,
                       as_stream(stream), c->view, a);
   }));
   return DKV_OK;

@@ -303,7 +303,7 @@ __device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, con
 // where there are blocks enough.  Angles are shared by all heads (shared memory, [R][rot/2]).  grid (pages a sequence can touch,
 // 2 Hkv / per, n); the last block of a sequence to arrive (a ticket) makes the rows part of it.
 constexpr int kQuadThreads = 512;                                            // R * D / 32 threads, at most
-template <int D, int kKind, int kIo>
+template <int D, int kKind, int kIo, bool kTurn>
 __global__ void __launch_bounds__(kQuadThreads)
 append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendArgs a) {
   extern __shared__ float2 turn_s[];
@@ -324,19 +324,21 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
   if (r0 < r1) {
     const int page = table[slot], y0 = blockIdx.y * a.per, y1 = min(2 * c.Hkv, y0 + a.per);
     struct Raw { uint4 v[4]; };
-    auto line = [&](int y, int k) {                                          // a new row of the source
-      const Rows8& src = y & 1 ? a.v : a.k;
-      return static_cast<const unsigned short*>(src.data) + i * src.batch + (y >> 1) * src.head + (base + quad_row(blk, t, k) - len) * src.token;
-    };
+    // the page's row 0 (which may lie before the source) in both tensors, and a quad's rows from there
+    const unsigned short* from_k = static_cast<const unsigned short*>(a.k.data) + i * a.k.batch + (base - len) * a.k.token;
+    const unsigned short* from_v = static_cast<const unsigned short*>(a.v.data) + i * a.v.batch + (base - len) * a.v.token;
+    const long long token_k = a.k.token, token_v = a.v.token, head_k = a.k.head, head_v = a.v.head;
     auto is_new = [&](int k) { return quad_row(blk, t, k) >= r0 && quad_row(blk, t, k) < r1; };
     auto ask = [&](int y) {
       Raw raw;
+      const long long token = y & 1 ? token_v : token_k;
+      const unsigned short* from = (y & 1 ? from_v + (y >> 1) * head_v : from_k + (y >> 1) * head_k) + d;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) raw.v[k] = is_new(k) ? *reinterpret_cast<const uint4*>(line(y, k) + d) : make_uint4(0, 0, 0, 0);
+      for (int k = 0; k < 4; ++k) raw.v[k] = is_new(k) ? *reinterpret_cast<const uint4*>(from + quad_row(blk, t, k) * token) : make_uint4(0, 0, 0, 0);
       return raw;
     };
     Raw raw = ask(y0);
-    if (a.rot) {
+    if (kTurn) {
       const int pos0 = a.pos0[i] + base - len;
       for (int x = tid; x < (r1 - r0) * (a.rot / 2); x += blockDim.x) {
         const int r = r0 + x / (a.rot / 2), pair = x % (a.rot / 2);
@@ -350,14 +352,14 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
       unsigned char* to = c.pages + reg * (size_t)(R * D);
       const Raw now = raw;
       if (y + 1 < y1) raw = ask(y + 1);
-      const bool turned = a.rot && !which;
+      const bool turned = kTurn && !which;
       Quad x;
       unsigned int bits = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         bits = largest_bits(bits, now.v[k]);
         x.row[k] = unpack8<kIo>(now.v[k]);
-        if (turned && is_new(k)) turn_row<kIo>(x.row[k], a, line(y, k), d, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
+        if (turned && is_new(k)) turn_row<kIo>(x.row[k], a, from_k + (y >> 1) * head_k + quad_row(blk, t, k) * token_k, d, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
       }
       float most = largest_of<kIo>(bits);
       bool odd = has_odd<kIo>(bits);
@@ -411,14 +413,14 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
   bool ok = true;
   for (int hw = threadIdx.x >> 5; ok && hw < 2 * c.Hkv; hw += blockDim.x >> 5) {
     const int h = hw >> 1, which = hw & 1;
-    const Rows8& src = which ? a.v : a.k;
-    const unsigned short* from = static_cast<const unsigned short*>(src.data) + i * src.batch + h * src.head;
+    const long long token = which ? a.v.token : a.k.token;
+    const unsigned short* from = static_cast<const unsigned short*>(which ? a.v.data : a.k.data) + i * (which ? a.v.batch : a.k.batch) + h * (which ? a.v.head : a.k.head);
     Eight x[kPer];
     uint4 raw[kPer];
 #pragma unroll
     for (int p = 0; p < kPer; ++p) {
       const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8;
-      raw[p] = j < a.cap ? *reinterpret_cast<const uint4*>(from + j * src.token + d) : make_uint4(0, 0, 0, 0);
+      raw[p] = j < a.cap ? *reinterpret_cast<const uint4*>(from + j * token + d) : make_uint4(0, 0, 0, 0);
     }
     const int pos0 = a.rot && !which ? a.pos0[i] : 0;
     const int not_ok = no_room(c, a, table, len, held, add);
@@ -431,7 +433,7 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
     for (int p = 0; p < kPer; ++p) {
       const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8;
       x[p] = unpack8<kIo>(raw[p]);
-      if (a.rot && !which && j < add) turn_row<kIo>(x[p], a, from + j * src.token, d, [&](int pair) { return turned_by(a, pos0 + j, pair); });
+      if (a.rot && !which && j < add) turn_row<kIo>(x[p], a, from + j * token, d, [&](int pair) { return turned_by(a, pos0 + j, pair); });
     }
     for (int base = len & -R; base < len + add; base += R) {
       const int r0 = max(0, len - base), r1 = min(R, len + add - base);
@@ -494,13 +496,14 @@ read8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ ReadArgs 
   const size_t reg = region(c, c.table[(size_t)seq * c.max_pages + blockIdx.x], h, which);
   const QuadWords w = get_words<D>(c.pages + reg * (size_t)(R * D), blk, t, d, which, rows);
   const float scale = c.scales[reg];
-  const Rows8& dst = which ? a.v : a.k;
-  unsigned short* to = static_cast<unsigned short*>(const_cast<void*>(dst.data)) + i * dst.batch + h * dst.head + d;
+  const long long token = which ? a.v.token : a.k.token;
+  unsigned short* to = static_cast<unsigned short*>(const_cast<void*>(which ? a.v.data : a.k.data)) + i * (which ? a.v.batch : a.k.batch) +
+                       h * (which ? a.v.head : a.k.head) + d;
   const Quad q = quad_of<kKind>(w, scale, which);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int r = quad_row(blk, t, k);
-    if (r < rows) *reinterpret_cast<uint4*>(to + (base + r) * dst.token) = pack8<kIo>(q.row[k]);
+    if (r < rows) *reinterpret_cast<uint4*>(to + (base + r) * token) = pack8<kIo>(q.row[k]);
   }
 }
 
