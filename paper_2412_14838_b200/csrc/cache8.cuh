@@ -228,9 +228,22 @@ struct AppendArgs {
   double turns[128];
 };
 
-// Turns eight dims d.. of a row; cs(i) gives (A cos, A sin) of pair i.
+// The largest magnitude of eight raw numbers so far, as bits of their type, two at a time: magnitudes order like integers, and
+// infinities and NaN are above all numbers.
+__device__ __forceinline__ unsigned int largest_bits(unsigned int most, uint4 v) {
+  return __vmaxu2(__vmaxu2(most, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu)), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+}
+template <int kIo>
+__device__ __forceinline__ bool has_odd(unsigned int bits) {       // an infinity or NaN among them
+  constexpr unsigned int inf = kIo == DKV_BF16 ? 0x7F80u : 0x7C00u;
+  return (bits & 0xFFFF) >= inf || bits >> 16 >= inf;
+}
+template <int kIo>
+__device__ __forceinline__ float largest_of(unsigned int bits) { return load16<kIo>((unsigned short)max(bits & 0xFFFF, bits >> 16)); }
+// Turns eight dims d.. of a row; cs(i) gives (A cos, A sin) of pair i.  bits: the largest magnitude of the raw numbers that were used
+// besides x's own, so far (largest_bits); all of them above, where they were not looked at.
 template <int kIo, typename F>
-__device__ __forceinline__ void turn_row(Eight& x, const AppendArgs& a, const unsigned short* line, int d, F cs) {
+__device__ __forceinline__ void turn_row(Eight& x, unsigned int& bits, const AppendArgs& a, const unsigned short* line, int d, F cs) {
   if (d >= a.rot) return;
   const int half = a.rot / 2;
   if (a.pairs) {
@@ -243,7 +256,13 @@ __device__ __forceinline__ void turn_row(Eight& x, const AppendArgs& a, const un
       }
   } else {
     Eight y;
-    if (a.vec) y = unpack8<kIo>(*reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half)));
+    if (a.vec) {
+      const uint4 raw = *reinterpret_cast<const uint4*>(line + (d < half ? d + half : d - half));
+      bits = largest_bits(bits, raw);
+      y = unpack8<kIo>(raw);
+    } else {
+      bits = 0x7FFF7FFFu;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (d + e < a.rot) {
@@ -259,18 +278,6 @@ __device__ __forceinline__ float2 turned_by(const AppendArgs& a, int pos, int pa
   turn_of(pos, a.turns[pair], c, s);
   return make_float2(a.amplitude * c, a.amplitude * s);
 }
-// The largest magnitude of eight raw numbers so far, as bits of their type, two at a time: magnitudes order like integers, and
-// infinities and NaN are above all numbers.
-__device__ __forceinline__ unsigned int largest_bits(unsigned int most, uint4 v) {
-  return __vmaxu2(__vmaxu2(most, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu)), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-}
-template <int kIo>
-__device__ __forceinline__ bool has_odd(unsigned int bits) {       // an infinity or NaN among them
-  constexpr unsigned int inf = kIo == DKV_BF16 ? 0x7F80u : 0x7C00u;
-  return (bits & 0xFFFF) >= inf || bits >> 16 >= inf;
-}
-template <int kIo>
-__device__ __forceinline__ float largest_of(unsigned int bits) { return load16<kIo>((unsigned short)max(bits & 0xFFFF, bits >> 16)); }
 // The largest finite magnitude of eight numbers; NaN becomes 0 and what is infinite the largest float.  Whether there were some.
 __device__ __forceinline__ bool settle(Eight& x, float& most) {
   bool odd = false;
@@ -359,11 +366,18 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
       for (int k = 0; k < 4; ++k) {
         bits = largest_bits(bits, now.v[k]);
         x.row[k] = unpack8<kIo>(now.v[k]);
-        if (turned && is_new(k)) turn_row<kIo>(x.row[k], a, from_k + (y >> 1) * head_k + quad_row(blk, t, k) * token_k, d, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
+        if (turned && is_new(k)) turn_row<kIo>(x.row[k], bits, a, from_k + (y >> 1) * head_k + quad_row(blk, t, k) * token_k, d, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
       }
       float most = largest_of<kIo>(bits);
-      bool odd = has_odd<kIo>(bits);
-      if (turned || odd) {                                                   // the numbers themselves: turned, or not all of them finite
+      bool odd = has_odd<kIo>(bits) || (turned && !(most * a.amplitude < 1e38f));       // turned numbers are at most twice as large: finite
+      if (turned && !odd) {
+        most = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
+      }
+      if (odd) {                                                             // some may not be finite
         most = 0.f;
         odd = false;
 #pragma unroll
@@ -433,7 +447,8 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
     for (int p = 0; p < kPer; ++p) {
       const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8;
       x[p] = unpack8<kIo>(raw[p]);
-      if (a.rot && !which && j < add) turn_row<kIo>(x[p], a, from + j * token, d, [&](int pair) { return turned_by(a, pos0 + j, pair); });
+      unsigned int bits = 0;
+      if (a.rot && !which && j < add) turn_row<kIo>(x[p], bits, a, from + j * token, d, [&](int pair) { return turned_by(a, pos0 + j, pair); });
     }
     for (int base = len & -R; base < len + add; base += R) {
       const int r0 = max(0, len - base), r1 = min(R, len + add - base);
@@ -720,7 +735,7 @@ struct CompactArgs {
 // need.  A quad of keys and one of values a thread, all their loads in flight.  A row's values lie in 32 bytes of every 128, so four
 // times their bytes are read.  grid (pages of `cols` rows, Hkv, n).
 template <int D, int kKind>
-__global__ void __launch_bounds__(kQuadThreads)
+__global__ void __launch_bounds__(kQuadThreads, 2)
 compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ CompactArgs a) {
   __shared__ float warp_s[2][kQuadThreads / 32];
   const int R = c.R, tid = threadIdx.x, h = blockIdx.y, i = blockIdx.z, seq = a.first + i * a.step;
