@@ -392,8 +392,8 @@ typedef struct {
 } dkv_cache8_config;
 typedef struct dkv_cache8 dkv_cache8;
 
-/* Create a cache without rows on the current device (host call; allocates n_pages * 2 * n_kv_heads * (R * head_dim + 4) bytes of pages,
- * 8 * n_seqs * max_pages of tables and, for dkv_cache8_attend, about 68 KB an SM).  It belongs to that device and to one stream at
+/* Create a cache without rows on the current device (host call; one allocation of n_pages * 2 * n_kv_heads * (R * head_dim + 4)
+ * bytes of pages, 8 * n_seqs * max_pages of tables, 1536 * (head_dim + 2) an SM for dkv_cache8_attend, and some per page and sequence).  It belongs to that device and to one stream at
  * a time: calls on it, replays of graphs that hold such calls included, follow one another.
  * Errors: INVALID_ARG, UNSUPPORTED, NOMEM, CUDA.  On error *out is NULL. */
 int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out);
@@ -443,10 +443,16 @@ int dkv_cache8_trim(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const
  * [n_seqs][max_pages] (the first held entries of each), refs int32 [n_pages] sequences that hold a page. */
 int dkv_cache8_views(dkv_cache8* c, const int32_t** len, const int32_t** held, const int32_t** table, const int32_t** refs);
 /* Synchronises the device.  host int32 [8]: [0] what went wrong since the last report, as bits: 1 no free pages, 2 more pages than a
- * sequence's table holds, 4 rows added without room, 8 a count or row number out of range, 16 an infinity or NaN was stored;
+ * sequence's table holds, 4 rows added without room, 8 a count or row number out of range, 16 an infinity or NaN was stored,
+ * 32 a wait inside dkv_cache8_attend ran out (its results are not to be used; the cache stays as it was);
  * [1] the lowest sequence concerned (-1: none), [2] free pages now, [3] low and [4] high half of the kernels launched.
- * Returns DKV_OK, DKV_ERR_NOMEM for bits 1 or 2, else DKV_ERR_STATE for bit 4, else DKV_ERR_INVALID_ARG for bit 8. */
+ * Returns DKV_OK, DKV_ERR_TIMEOUT for bit 32, else DKV_ERR_NOMEM for bits 1 or 2, else DKV_ERR_STATE for bit 4, else DKV_ERR_INVALID_ARG for bit 8. */
 int dkv_cache8_status(dkv_cache8* c, int32_t* host_status);
+/* As dkv_set_wait_limit, for the waits inside dkv_cache8_attend (default 4e9 clock ticks, at least 1000). */
+int dkv_cache8_set_wait_limit(dkv_cache8* c, int64_t clock_ticks);
+/* Test hook for the path above: in the dkv_cache8_attend calls that follow, warp 0 of thread block 0 never asks for its chunk
+ * number `chunk` (0-based, 32 rows each), so that the wait for it runs out.  chunk < 0 switches the hook off.  Nothing else is disturbed. */
+int dkv_cache8_debug_withhold(dkv_cache8* c, int32_t chunk);
 /* CUDA error code of the last DKV_ERR_CUDA on this cache (0 = none). */
 int dkv_cache8_last_cuda_error(dkv_cache8* c);
 

@@ -25,7 +25,7 @@ EXPORTS = [
     "dkv_static_last_status", "dkv_set_wait_limit", "dkv_debug_withhold_tile", "dkv_profile", "dkv_profile_read", "dkv_launch_count", "dkv_last_cuda_error",
     "dkv_strerror", "dkv_version", "dkv_rotary_init", "dkv_rotate", "dkv_cache8_create", "dkv_cache8_destroy", "dkv_cache8_reserve",
     "dkv_cache8_append", "dkv_cache8_read", "dkv_cache8_attend", "dkv_cache8_fork", "dkv_cache8_compact", "dkv_cache8_trim",
-    "dkv_cache8_views", "dkv_cache8_status", "dkv_cache8_last_cuda_error",
+    "dkv_cache8_views", "dkv_cache8_status", "dkv_cache8_set_wait_limit", "dkv_cache8_debug_withhold", "dkv_cache8_last_cuda_error",
 ]
 
 DKV_OK, DKV_ERR_INVALID_ARG, DKV_ERR_STATE, DKV_ERR_CUDA = 0, -1, -2, -3
@@ -126,6 +126,8 @@ def load() -> ctypes.CDLL:
         "dkv_cache8_trim": [vp, i32, i32, i32, vp, i32, vp],
         "dkv_cache8_views": [vp, pp, pp, pp, pp],
         "dkv_cache8_status": [vp, vp],
+        "dkv_cache8_set_wait_limit": [vp, ctypes.c_int64],
+        "dkv_cache8_debug_withhold": [vp, i32],
         "dkv_cache8_last_cuda_error": [vp],
     }
     for name, args in sig.items():
@@ -403,7 +405,7 @@ DKV_ROTARY_HALF, DKV_ROTARY_PAIRS = 0, 1
 DKV_SCALING_NONE, DKV_SCALING_LINEAR, DKV_SCALING_BASE, DKV_SCALING_WAVELENGTH, DKV_SCALING_RAMP = 0, 1, 2, 3, 4
 DKV_E4M3, DKV_INT8 = 0, 1
 #: Bits of dkv_cache8_status's first word.
-DKV_C8_NO_PAGES, DKV_C8_TABLE_FULL, DKV_C8_NO_ROOM, DKV_C8_BAD_ARGUMENT, DKV_C8_NOT_FINITE = 1, 2, 4, 8, 16
+DKV_C8_NO_PAGES, DKV_C8_TABLE_FULL, DKV_C8_NO_ROOM, DKV_C8_BAD_ARGUMENT, DKV_C8_NOT_FINITE, DKV_C8_TIMEOUT = 1, 2, 4, 8, 16, 32
 
 
 def _struct(x):
@@ -486,6 +488,14 @@ def dkv_cache8_status(cache: int):
     buf = (ctypes.c_int32 * 8)()
     code = load().dkv_cache8_status(cache, buf)
     return code, list(buf)
+
+
+def dkv_cache8_set_wait_limit(cache: int, clock_ticks: int) -> None:
+    _check(load().dkv_cache8_set_wait_limit(cache, clock_ticks), "dkv_cache8_set_wait_limit")
+
+
+def dkv_cache8_debug_withhold(cache: int, chunk: int) -> None:
+    _check(load().dkv_cache8_debug_withhold(cache, chunk), "dkv_cache8_debug_withhold")
 
 
 def dkv_cache8_last_cuda_error(cache: int) -> int:

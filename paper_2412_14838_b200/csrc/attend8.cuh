@@ -21,7 +21,7 @@ namespace dkv {
 
 constexpr int kAttendWarps = 12, kAttendStages = 2, kAttendRows = 32;
 constexpr int kAttendMaxSeqs = 1024;        // sequences a launch (their lengths and groups' prefix sums are in shared memory)
-constexpr long long kAttendWait = 4000000000ll;  // clock ticks after which a wait for a copy gives up, about 2 s
+constexpr float kDown = 5.9604644775390625e-8f;  // 2^-24: results are summed that much smaller, so that values up to the largest bf16 numbers sum without overflow
 constexpr float kLift = 8.f, kSlack = 7.f;  // weights are 2^(logit - reference + kLift); logits may pass the reference by kSlack: 2^15 fits fp16
 
 struct AttendArgs {
@@ -32,6 +32,8 @@ struct AttendArgs {
   float* lse;                // [n][Hq][nq] or null
   float* scratch;            // [2 slices][rows of a head, in whole QB] partial results, (reference, sum) behind them
   unsigned int* tickets;     // [n * Hkv], zero between launches
+  long long wait;            // clock ticks after which a wait for a copy gives up
+  int withhold;              // test hook: the chunk that warp 0 of block 0 never asks for, -1: none
   int first, step, n, nq, rows, G, causal, slots, io;
   float scale2;              // log2(e) / sqrt(D)
 };
@@ -73,6 +75,8 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
   return sum == 0.f ? -INFINITY : (ref - kLift + log2f(sum)) * 0.6931471805599453f;
 }
 
+// What takes a sum of weighted values to the result; a query that sees no row has sums of 0.
+__device__ __forceinline__ float up(float sum) { return sum == 0.f ? 0.f : 1.f / (kDown * sum); }
 __device__ __forceinline__ float* out_row(const AttendArgs& a, int i, int h, int row) { return a.out + i * a.out_batch + (h * a.G + row / a.nq) * a.out_head + row % a.nq * a.out_token; }
 __device__ __forceinline__ void store_lse(const AttendArgs& a, int Hkv, int i, int h, int row, float ref, float sum) {
   if (a.lse) a.lse[((size_t)(i * Hkv + h) * a.G + row / a.nq) * a.nq + row % a.nq] = log_sum(ref, sum);
@@ -311,7 +315,7 @@ struct AttendWarp {
     for (int k = 0; k < kHalves; ++k) {
       const int row = g + 8 * k;
       if (row >= a.rows) continue;
-      const float inv = sum[k] == 0.f ? 0.f : 1.f / sum[k];
+      const float inv = up(sum[k]);
       float* to = out_row(a, i, h, row);
       if (t == 0) store_lse(a, Hkv, i, h, row, ref[k], sum[k]);
 #pragma unroll
@@ -340,9 +344,9 @@ __device__ __forceinline__ bool ring_done(uint32_t bar, uint32_t parity) {
   asm volatile("{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, long long limit) {
   if (ring_done(bar, parity)) return true;
-  for (const long long t0 = clock64(); clock64() - t0 < kAttendWait;)
+  for (const long long t0 = clock64(); clock64() - t0 < limit;)
     if (ring_done(bar, parity)) return true;
   return false;
 }
@@ -353,11 +357,14 @@ struct Ring {
   static constexpr int kHalfBytes = kAttendRows * D, kChunkBytes = 2 * kHalfBytes, kBytes = kAttendStages * kChunkBytes;
   unsigned char* at;
   uint32_t at_s, bar_s;
+  long long limit;
   int stage = 0, phase = 0;                            // of the next chunk that is waited for
+  int withhold;
   bool broken = false;                                 // a wait ran out: nothing more is asked for or waited for
 
-  __device__ __forceinline__ void start(unsigned char* ring, unsigned long long* bars, int lane) {
-    at = ring;
+  __device__ __forceinline__ void start(unsigned char* ring, unsigned long long* bars, int lane, const AttendArgs& a) {
+    at = ring; limit = a.wait;
+    withhold = blockIdx.x == 0 && threadIdx.x < 32 ? a.withhold : -1;
     at_s = (uint32_t)__cvta_generic_to_shared(ring); bar_s = (uint32_t)__cvta_generic_to_shared(bars);
     if (lane == 0) {
       for (int i = 0; i < kAttendStages; ++i) ring_init(bar_s + i * 8);
@@ -368,7 +375,7 @@ struct Ring {
   // What is still on its way ends before the block does.
   __device__ __forceinline__ void finish() {
     if (broken)
-      for (int i = 0; i < kAttendStages; ++i) ring_wait(bar_s + i * 8, i < stage ? phase ^ 1 : phase);
+      for (int i = 0; i < kAttendStages; ++i) ring_wait(bar_s + i * 8, i < stage ? phase ^ 1 : phase, limit);
   }
   // Adds `count` chunks of head h to w: chunk x is rows first + 32 step x and on.
   template <int QB, int kKind>
@@ -391,6 +398,7 @@ struct Ring {
         const unsigned char* k = c.pages + region(c, p, h, 0) * (size_t)(c.R * D) + (row & (c.R - 1)) * D;
         const uint32_t bar = bar_s + into * 8, to = at_s + into * kChunkBytes;
         ring_expect(bar, kChunkBytes);
+        if (withhold-- == 0) return;
         if (c.R == kAttendRows) ring_copy(to, k, kChunkBytes, bar);
         else { ring_copy(to, k, kHalfBytes, bar); ring_copy(to + kHalfBytes, k + c.R * D, kHalfBytes, bar); }
       }
@@ -405,8 +413,8 @@ struct Ring {
       if (((x + kAttendStages - 1) & 31) == 0) look(x + kAttendStages - 1);
       __syncwarp();                                    // every lane is done with the place that is filled next
       fetch(x + kAttendStages - 1, (stage + kAttendStages - 1) % kAttendStages);
-      if (!broken) broken = !__all_sync(0xFFFFFFFFu, ring_wait(bar_s + stage * 8, phase));
-      const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
+      if (!broken) broken = !__all_sync(0xFFFFFFFFu, ring_wait(bar_s + stage * 8, phase, limit));
+      const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = kDown * __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
       const unsigned char* k = at + stage * kChunkBytes;
       if (!broken) w.add(reinterpret_cast<const uint4*>(k), reinterpret_cast<const uint4*>(k + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, first + x * step * kAttendRows, lane, t);
       if (++stage == kAttendStages) { stage = 0; phase ^= 1; }
@@ -468,7 +476,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
   float* part_s = reinterpret_cast<float*>(smem);
   float2* ml_s = reinterpret_cast<float2*>(part_s + NW * QB * (D + 4));
   pdl_launch();
-  ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane);
+  ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane, a);
   pdl_wait();
   sum_units(c, a, len_s, prefix_s, scan_s, [](int len) { return max(1, (chunks_of(len) + NW - 1) / NW); });
   // as many slices a head as there can be, and no slice in two heads, where that leaves few blocks without one
@@ -504,7 +512,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
         const float2 ml = merge_warps<D, QB, NW>(part_s, ml_s, x, v);
         const int qi = x / (D / 4), d = x % (D / 4) * 4;
         if (whole) {
-          const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
+          const float inv = up(ml.y);
           *reinterpret_cast<float4*>(out_row(a, lo, h, c0 + qi) + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
           if (d == 0) store_lse(a, c.Hkv, lo, h, c0 + qi, ml.x, ml.y);
         } else {
@@ -543,7 +551,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
         for (int p = lane; p < parts; p += 32) l += weight(all_s[p * QB + qi]) * all_s[p * QB + qi].y;
 #pragma unroll
         for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = up(l);
         for (int p = lane; p < parts; p += 32) weight_s[p * QB + qi] = weight(all_s[p * QB + qi]) * inv;
         if (lane == 0) store_lse(a, c.Hkv, lo, h, c0 + qi, m, l);
       }
@@ -594,7 +602,7 @@ attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ A
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   Ring<D> ring;
   pdl_launch();
-  ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane);
+  ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane, a);
   pdl_wait();
   sum_units(c, a, len_s, prefix_s, scan_s, [](int len) { return chunks_of(len) + kAttendHeadCost; });
   // no more slices than units: an empty slice would leave no part, and whoever merges a head counts on one from each

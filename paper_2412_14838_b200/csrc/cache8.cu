@@ -10,6 +10,7 @@
 #include <atomic>
 #include <new>
 #include <type_traits>
+#include <utility>
 #include <vector>
 
 #include "../../include/dkv.h"
@@ -28,7 +29,10 @@ struct dkv_cache8 {
   unsigned int* d_tickets;      // [n_seqs * Hkv], zero between launches
   float* d_scratch;             // parts of heads that lie in several blocks' slices
   long long launches;
+  long long wait_cycles;        // dkv_cache8_set_wait_limit
+  int withhold;                 // dkv_cache8_debug_withhold
   int last_cuda;
+  void* memory;                 // all of the above
 };
 
 namespace {
@@ -109,15 +113,6 @@ int validate(const dkv_cache8_config* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return DKV_ERR_UNSUPPORTED;
   if (c->page_rows != 32 && c->page_rows != 64 && c->page_rows != 128) return DKV_ERR_UNSUPPORTED;
   if (c->n_pages > 1 << 26 || c->n_seqs > 65535 || c->n_kv_heads > 32767 || (long long)c->max_pages * c->page_rows > 1 << 24) return DKV_ERR_UNSUPPORTED;
-  return DKV_OK;
-}
-
-int free_cache(dkv_cache8* c) {
-  for (void* p : {(void*)c->view.pages, (void*)c->view.scales, (void*)c->view.table, (void*)c->view.len, (void*)c->view.held, (void*)c->view.refs,
-                  (void*)c->view.free, (void*)c->view.hint, (void*)c->view.status, (void*)c->d_pick, (void*)c->d_jobs,
-                  (void*)c->d_new_table, (void*)c->d_new_held, (void*)c->d_tickets, (void*)c->d_scratch})
-    cudaFree(p);
-  delete c;
   return DKV_OK;
 }
 
@@ -273,36 +268,39 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
   Cache8& v = c->view;
   v.Hkv = cfg->n_kv_heads; v.D = cfg->head_dim; v.R = cfg->page_rows; v.max_pages = cfg->max_pages; v.n_pages = cfg->n_pages;
   v.shift = cfg->page_rows == 32 ? 5 : cfg->page_rows == 64 ? 6 : 7;
+  c->wait_cycles = 4000000000ll;               // about 2 s
+  c->withhold = -1;
   const size_t regions = (size_t)cfg->n_pages * cfg->n_kv_heads * 2, entries = (size_t)cfg->n_seqs * cfg->max_pages;
   const int words = (cfg->n_pages + 31) / 32;
   cudaError_t e = cudaGetDevice(&c->device);
 #define TRY(call) if (e == cudaSuccess) e = (call)
   TRY(cudaDeviceGetAttribute(&c->n_sms, cudaDevAttrMultiProcessorCount, c->device));
-  TRY(cudaMalloc(&v.pages, regions * cfg->page_rows * cfg->head_dim));
-  TRY(cudaMalloc(&v.scales, regions * sizeof(float)));
-  TRY(cudaMalloc(&v.table, entries * sizeof(int)));
-  TRY(cudaMalloc(&v.len, sizeof(int) * cfg->n_seqs));
-  TRY(cudaMalloc(&v.held, sizeof(int) * cfg->n_seqs));
-  TRY(cudaMalloc(&v.refs, sizeof(int) * cfg->n_pages));
-  TRY(cudaMalloc(&v.free, sizeof(int) * words));
-  TRY(cudaMalloc(&v.hint, sizeof(int)));
-  TRY(cudaMalloc(&v.status, sizeof(int) * 2));
-  TRY(cudaMalloc(&c->d_pick, sizeof(int) * cfg->n_pages));
-  TRY(cudaMalloc(&c->d_jobs, sizeof(int) * (1 + 2 * cfg->n_seqs)));
-  TRY(cudaMalloc(&c->d_new_table, entries * sizeof(int)));
-  TRY(cudaMalloc(&c->d_new_held, sizeof(int) * cfg->n_seqs));
-  TRY(cudaMalloc(&c->d_tickets, sizeof(int) * (size_t)cfg->n_seqs * cfg->n_kv_heads));
-  TRY(cudaMalloc(&c->d_scratch, sizeof(float) * attend_scratch(c)));
-  // every code is a number from the start: what rows not yet written hold is multiplied by a weight of zero
-  TRY(cudaMemset(v.pages, 0, regions * cfg->page_rows * cfg->head_dim));
-  TRY(cudaMemset(v.scales, 0, regions * sizeof(float)));
-  TRY(cudaMemset(v.table, 0, entries * sizeof(int)));
-  TRY(cudaMemset(v.len, 0, sizeof(int) * cfg->n_seqs));
-  TRY(cudaMemset(v.held, 0, sizeof(int) * cfg->n_seqs));
-  TRY(cudaMemset(v.refs, 0, sizeof(int) * cfg->n_pages));
-  TRY(cudaMemset(v.hint, 0, sizeof(int)));
-  TRY(cudaMemset(c->d_jobs, 0, sizeof(int) * (1 + 2 * cfg->n_seqs)));
-  TRY(cudaMemset(c->d_tickets, 0, sizeof(int) * (size_t)cfg->n_seqs * cfg->n_kv_heads));
+  // one allocation: every part on a 256-byte boundary, zeros but for what follows below.  Every code is a number from the start:
+  // what rows not yet written hold is multiplied by a weight of zero
+  size_t bytes = 0;
+  std::vector<std::pair<void**, size_t>> parts;
+  auto part = [&](auto& p, size_t n) { parts.push_back({reinterpret_cast<void**>(&p), bytes}); bytes += (n * sizeof *p + 255) / 256 * 256; };
+  try {
+    part(v.pages, regions * cfg->page_rows * cfg->head_dim);
+    part(v.scales, regions);
+    part(v.table, entries);
+    part(v.len, cfg->n_seqs);
+    part(v.held, cfg->n_seqs);
+    part(v.refs, cfg->n_pages);
+    part(v.free, words);
+    part(v.hint, 1);
+    part(v.status, 2);
+    part(c->d_pick, cfg->n_pages);
+    part(c->d_jobs, 1 + 2 * (size_t)cfg->n_seqs);
+    part(c->d_new_table, entries);
+    part(c->d_new_held, cfg->n_seqs);
+    part(c->d_tickets, (size_t)cfg->n_seqs * cfg->n_kv_heads);
+    part(c->d_scratch, attend_scratch(c));
+  } catch (const std::bad_alloc&) { delete c; return DKV_ERR_NOMEM; }
+  TRY(cudaMalloc(&c->memory, bytes));
+  if (e == cudaSuccess)
+    for (const auto& p : parts) *p.first = static_cast<char*>(c->memory) + p.second;
+  TRY(cudaMemset(c->memory, 0, bytes));
   if (e == cudaSuccess) {
     const int status[2] = {0, INT_MAX};
     e = cudaMemcpy(v.status, status, sizeof status, cudaMemcpyHostToDevice);
@@ -321,7 +319,8 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
 #undef TRY
   if (e != cudaSuccess) {
     cudaGetLastError();
-    free_cache(c);
+    cudaFree(c->memory);
+    delete c;
     return e == cudaErrorMemoryAllocation ? DKV_ERR_NOMEM : DKV_ERR_CUDA;
   }
   *out = c;
@@ -331,7 +330,9 @@ int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out) {
 int dkv_cache8_destroy(dkv_cache8* c) {
   if (!c) return DKV_ERR_INVALID_ARG;
   cudaDeviceSynchronize();
-  return free_cache(c);
+  cudaFree(c->memory);
+  delete c;
+  return DKV_OK;
 }
 
 int dkv_cache8_reserve(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* rows, int32_t add, void* stream) {
@@ -397,7 +398,7 @@ int dkv_cache8_attend(dkv_cache8* c, int32_t first, int32_t n, int32_t step, con
   a.q_batch = q->batch_stride; a.q_head = q->head_stride; a.q_token = q->token_stride;
   a.out_batch = out->batch_stride; a.out_head = out->head_stride; a.out_token = out->token_stride;
   a.scratch = c->d_scratch; a.tickets = c->d_tickets;
-  a.step = step; a.nq = q->tokens; a.rows = G * q->tokens; a.G = G; a.causal = causal != 0; a.io = c->cfg.io;
+  a.step = step; a.nq = q->tokens; a.rows = G * q->tokens; a.G = G; a.causal = causal != 0; a.io = c->cfg.io; a.wait = c->wait_cycles; a.withhold = c->withhold;
   a.slots = (a.rows + (a.rows <= 8 ? 7 : 15)) / (a.rows <= 8 ? 8 : 16);
   a.scale2 = kLog2e / sqrtf((float)c->cfg.head_dim);
   // sequences a launch: their prefix sums fit shared memory, and their units (chunks, at most) 31 bits
@@ -478,6 +479,18 @@ int dkv_cache8_status(dkv_cache8* c, int32_t* host_status) {
   if (status[0] & kTimeout) return DKV_ERR_TIMEOUT;
   if (status[0] & (kNoPages | kTableFull)) return DKV_ERR_NOMEM;
   return status[0] & kNoRoom ? DKV_ERR_STATE : status[0] & kBadArgument ? DKV_ERR_INVALID_ARG : DKV_OK;
+}
+
+int dkv_cache8_set_wait_limit(dkv_cache8* c, int64_t clock_ticks) {
+  if (!c || clock_ticks < 1000) return DKV_ERR_INVALID_ARG;
+  c->wait_cycles = clock_ticks;
+  return DKV_OK;
+}
+
+int dkv_cache8_debug_withhold(dkv_cache8* c, int32_t chunk) {
+  if (!c) return DKV_ERR_INVALID_ARG;
+  c->withhold = chunk < 0 ? -1 : chunk;
+  return DKV_OK;
 }
 
 int dkv_cache8_last_cuda_error(dkv_cache8* c) { return c ? c->last_cuda : 0; }

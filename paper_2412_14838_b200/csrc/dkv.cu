@@ -694,7 +694,7 @@ int ensure_staging(dkv_ctx* c) {
 
 extern "C" {
 
-int dkv_version(void) { return 1000; }
+int dkv_version(void) { return 1001; }
 
 const char* dkv_strerror(int code) {
   switch (code) {

@@ -219,6 +219,57 @@ def test_attention_over_larger_pages(R, kind):
         c.attend(0, 3, 1, 2, True)
 
 
+@pytest.mark.parametrize("kind,io", KINDS)
+@pytest.mark.parametrize("G,nq", [(4, 1), (5, 3), (6, 3)])                  # one pass of 8, one of 16, two: another division of the work
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_many_heads(kind, io, G, nq, D):
+    lens = [0, 1, 32, 33, 500] + [(i * 97) % 400 for i in range(35)]
+    with Both(n_pages=400, n_seqs=40, max_pages=20, D=D, kind=kind, io=io, G=G, Hkv=3) as c:
+        c.add(0, 40, 1, lens, G)
+        c.attend(0, 40, 1, nq, True)
+
+
+def test_a_long_sequence_lies_in_every_block():
+    with Both(n_pages=700, n_seqs=1, max_pages=700, D=64, Hkv=1, G=4, R=128) as c:
+        c.add(0, 1, 1, [65000], 1)                                           # 170 groups of twelve chunks: a slice of one or two each
+        c.attend(0, 1, 1, 1, False)
+        c.attend(0, 1, 1, 16, True)
+
+
+@pytest.mark.parametrize("size", [3e38, 1e-25])
+def test_values_at_the_ends_of_bf16(size):
+    with Both(n_pages=30, n_seqs=1, max_pages=30) as c:
+        k = torch.randn(1, 2, 300, 64, device="cuda").to(torch.bfloat16)
+        v = (torch.rand(1, 2, 300, 64, device="cuda") * size).to(torch.bfloat16)
+        B.dkv_cache8_reserve(c.h, 0, 1, 1, None, 300)
+        B.dkv_cache8_append(c.h, 0, 1, 1, k, v)
+        c.o.reserve([0], [300])
+        c.o.append(0, k[0].double().cpu().numpy(), v[0].double().cpu().numpy())
+        c.attend(0, 1, 1, 2, False)
+
+
+@pytest.mark.parametrize("n,Hkv", [(1, 2), (60, 2)])                        # a slice a block, a slice a warp
+@pytest.mark.parametrize("chunk", [0, 1])
+def test_a_wait_that_runs_out_is_reported_and_leaves_the_cache_usable(n, Hkv, chunk):
+    with Both(n_pages=4000, n_seqs=n, max_pages=900 // n * 4 + 20, Hkv=Hkv) as c:
+        rows = 60000 if n == 1 else 2000                                     # so many that the first warp has two chunks
+        c.add(0, n, 1, [rows] * n, 1)
+        q = torch.randn(n, Hkv * 2, 1, 64, device="cuda").to(torch.bfloat16)
+        out = torch.zeros(n, Hkv * 2, 1, 64, device="cuda")
+        B.dkv_cache8_attend(c.h, 0, n, 1, q, out)
+        good = out.clone()
+        B.dkv_cache8_set_wait_limit(c.h, 2_000_000)                          # about a millisecond
+        B.dkv_cache8_debug_withhold(c.h, chunk)
+        B.dkv_cache8_attend(c.h, 0, n, 1, q, out)
+        code, words = B.dkv_cache8_status(c.h)
+        assert code == B.DKV_ERR_TIMEOUT and words[0] == B.DKV_C8_TIMEOUT and words[1] == 0
+        B.dkv_cache8_debug_withhold(c.h, -1)
+        B.dkv_cache8_attend(c.h, 0, n, 1, q, out)
+        assert torch.equal(out, good) and B.dkv_cache8_status(c.h)[0] == B.DKV_OK
+        with pytest.raises(B.DkvError):
+            B.dkv_cache8_set_wait_limit(c.h, 10)
+
+
 def test_values_of_very_different_sizes_and_large_logits():
     with Both(n_pages=60, n_seqs=2, max_pages=30, D=128) as c:
         for i, scale in enumerate([1e-3, 1.0, 1e4, 1e-6, 30.0]):             # pages whose scales differ by 2^33
