@@ -456,74 +456,93 @@ __device__ __forceinline__ HeadAt head_at(int u, const int* prefix_s, int n, int
   const int units = (prefix_s[lo + 1] - prefix_s[lo]) / Hkv, h = (u - prefix_s[lo]) / units;
   return {lo, h, prefix_s[lo] + h * units, units};
 }
-// Few heads.  The rows of every (sequence, head) are taken in chunks of 32, kAttendWarps chunks a group, the groups of all heads as one
-// sequence that is cut into one equal slice a block; a head with one group is never cut.  In a slice the warps deal the chunks of a
-// head out among themselves and merge through shared memory; a head that lies in several slices is merged by the block that arrives
-// last (a ticket a head), in slice order, so that nothing depends on which that is.
-template <int D, int QB, int kKind>
+// As merge_warps, for `count` results: dims d .. d + 3 of query row qi.
+template <int D, int QB>
+__device__ __forceinline__ float2 merge_team(const float* part, const float2* ml, int count, int qi, int d, float4& v) {
+  float m = -INFINITY, l = 0.f;
+  for (int w = 0; w < count; ++w) m = fmaxf(m, ml[w * QB + qi].x);
+  v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int w = 0; w < count; ++w) {
+    const float2 p = ml[w * QB + qi];
+    const float k = p.y == 0.f ? 0.f : fast_exp2(p.x - m);                    // (a warp may have no row that this query sees)
+    const float4 y = *reinterpret_cast<const float4*>(part + (w * QB + qi) * (D + 4) + d);
+    v.x = fmaf(y.x, k, v.x); v.y = fmaf(y.y, k, v.y); v.z = fmaf(y.z, k, v.z); v.w = fmaf(y.w, k, v.w);
+    l = fmaf(p.y, k, l);
+  }
+  return make_float2(m, l);
+}
+
+// Few heads.  The warps of a block form a team for every QB query rows (one team of twelve for up to 16 rows, four of three for 64):
+// each team goes over the same rows of a head, which the others then find in L2.  The rows of every (sequence, head) are taken in
+// chunks of 32, a group as many chunks as a team has warps, the groups of all heads as one sequence that is cut into one equal
+// slice a block; a head with one group is never cut.  In a slice a team's warps deal the chunks of a head out among themselves and
+// merge through shared memory; a head that lies in several slices is merged by the block that arrives last (a ticket a head), in
+// slice order, so that nothing depends on which that is.  kTeams: more than one team.
+template <int D, int QB, int kKind, bool kTeams>
 __global__ void __launch_bounds__(kAttendWarps * 32, 1)
 attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendArgs a) {
   using Warp = AttendWarp<D, QB, kKind>;
   constexpr int NW = kAttendWarps;
   static_assert(NW * QB * (D + 4) * 4 + NW * QB * 8 <= attend_smem<D>() && 256 * QB * 12 <= attend_smem<D>());   // merges, of at most 256 parts
+  static_assert(NW % 2 == 0 && NW % 3 == 0 && NW % 4 == 0);                                                      // teams of equal size
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ int prefix_s[kAttendMaxSeqs + 1], len_s[kAttendMaxSeqs];
   __shared__ int scan_s[NW];
   __shared__ unsigned int ticket_s;
   __shared__ __align__(8) unsigned long long bar_s[NW * kAttendStages];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int teams = kTeams ? a.slots : 1, size = NW / teams;
+  const int c0 = kTeams ? warp / size * QB : 0, member = kTeams ? warp % size : warp;             // this warp's first query row, and place in its team
   Ring<D> ring;
   float* part_s = reinterpret_cast<float*>(smem);
   float2* ml_s = reinterpret_cast<float2*>(part_s + NW * QB * (D + 4));
   pdl_launch();
   ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane, a);
   pdl_wait();
-  sum_units(c, a, len_s, prefix_s, scan_s, [](int len) { return max(1, (chunks_of(len) + NW - 1) / NW); });
+  sum_units(c, a, len_s, prefix_s, scan_s, [&](int len) { return max(1, (chunks_of(len) + size - 1) / size); });
   // as many slices a head as there can be, and no slice in two heads, where that leaves few blocks without one
   const int total = prefix_s[a.n], heads = a.n * c.Hkv, even = gridDim.x - gridDim.x % heads;
   const Slices slices = {total, min(heads <= (int)gridDim.x && even * 8 >= (int)gridDim.x * 7 ? even : (int)gridDim.x, total)};
   const int own = blockIdx.x;
   if (own >= slices.count) return;
-  const int u1 = slices.begin(own + 1), passes = (a.rows + QB - 1) / QB;
+  const int u1 = slices.begin(own + 1);
   for (int u = slices.begin(own); u < u1;) {
     const HeadAt at = head_at(u, prefix_s, a.n, c.Hkv);
     const int lo = at.i, h = at.h, seq = a.first + lo * a.step, len = len_s[lo], end = min(u1, at.u0 + at.units);
-    const int ch0 = (u - at.u0) * NW, ch1 = min(chunks_of(len), (end - at.u0) * NW);
+    const int ch0 = (u - at.u0) * size, ch1 = min(chunks_of(len), (end - at.u0) * size);
     const bool begins = u == at.u0, whole = begins && end == at.u0 + at.units;
-    const int* table = c.table + (size_t)seq * c.max_pages;
     u = end;
     const int c_lo = slices.owner(at.u0), c_hi = slices.owner(at.u0 + at.units - 1);
     // parts: slot 0 of a slice continues a head, slot 1 begins one that others continue
-    auto part = [&](int sl, bool first, int pass) { return a.scratch + ((size_t)(2 * sl + first) * a.slots + pass) * (QB * (D + 2)); };
-    for (int pass = 0; pass < passes; ++pass) {
+    auto part = [&](int sl, bool first, int team) { return a.scratch + ((size_t)(2 * sl + first) * teams + team) * (QB * (D + 2)); };
+    {
       Warp w;
       typename Warp::Raw raw;
-      const int c0 = pass * QB, mine = max(0, (ch1 - ch0 - warp + NW - 1) / NW);      // this warp's chunks: ch0 + warp + NW x
+      const int mine = max(0, (ch1 - ch0 - member + size - 1) / size);       // this warp's chunks: ch0 + member + size x
       Warp::ask(raw, a, lo, h, c0, g, t);
-      ring.run(w, raw, c, a, table, h, c0, len, (ch0 + warp) * kAttendRows, NW, mine, lane, g, t);
+      ring.run(w, raw, c, a, c.table + (size_t)seq * c.max_pages, h, c0, len, (ch0 + member) * kAttendRows, size, mine, lane, g, t);
       if (ring.broken && lane == 0) report(c, kTimeout, seq);
       __syncthreads();
       w.add_up();
       w.park(part_s + warp * QB * (D + 4), ml_s + warp * QB, g, t);
-      __syncthreads();
-      const int pieces = min(QB, a.rows - c0) * (D / 4);
-      for (int x = tid; x < pieces; x += NW * 32) {
-        float4 v;
-        const float2 ml = merge_warps<D, QB, NW>(part_s, ml_s, x, v);
-        const int qi = x / (D / 4), d = x % (D / 4) * 4;
-        if (whole) {
-          const float inv = up(ml.y);
-          *reinterpret_cast<float4*>(out_row(a, lo, h, c0 + qi) + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-          if (d == 0) store_lse(a, c.Hkv, lo, h, c0 + qi, ml.x, ml.y);
-        } else {
-          float* to = part(own, begins, pass);
-          __stcg(reinterpret_cast<float4*>(to) + x, v);
-          if (d == 0) __stcg(reinterpret_cast<float2*>(to + QB * D) + qi, ml);
-        }
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the ring's copies come after what was written here
-      __syncthreads();
     }
+    __syncthreads();
+    for (int x = tid; x < a.rows * (D / 4); x += NW * 32) {
+      const int row = x / (D / 4), d = x % (D / 4) * 4, team = row / QB, qi = row % QB;
+      float4 v;
+      const float2 ml = kTeams ? merge_team<D, QB>(part_s + team * size * QB * (D + 4), ml_s + team * size * QB, size, qi, d, v) : merge_warps<D, QB, NW>(part_s, ml_s, x, v);
+      if (whole) {
+        const float inv = up(ml.y);
+        *reinterpret_cast<float4*>(out_row(a, lo, h, row) + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        if (d == 0) store_lse(a, c.Hkv, lo, h, row, ml.x, ml.y);
+      } else {
+        float* to = part(own, begins, team);
+        __stcg(reinterpret_cast<float4*>(to) + qi * (D / 4) + d / 4, v);
+        if (d == 0) __stcg(reinterpret_cast<float2*>(to + QB * D) + qi, ml);
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the ring's copies come after what was written here
+    __syncthreads();
     if (whole) continue;
     unsigned int* ticket = a.tickets + (size_t)lo * c.Hkv + h;
     if (tid == 0) {
@@ -537,10 +556,10 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
     const int parts = c_hi - c_lo + 1;
     float* weight_s = reinterpret_cast<float*>(smem);
     float2* all_s = reinterpret_cast<float2*>(weight_s + parts * QB);
-    for (int pass = 0; pass < passes; ++pass) {
-      const int c0 = pass * QB, rows = min(QB, a.rows - c0);
+    for (int team = 0; team < teams; ++team) {
+      const int r0 = team * QB, rows = min(QB, a.rows - r0);
       for (int x = tid; x < parts * QB; x += NW * 32)
-        if (x % QB < rows) all_s[x] = __ldcg(reinterpret_cast<const float2*>(part(c_lo + x / QB, x < QB, pass) + QB * D) + x % QB);
+        if (x % QB < rows) all_s[x] = __ldcg(reinterpret_cast<const float2*>(part(c_lo + x / QB, x < QB, team) + QB * D) + x % QB);
       __syncthreads();
       for (int qi = warp; qi < rows; qi += NW) {
         float m = -INFINITY, l = 0.f;
@@ -553,7 +572,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
         for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
         const float inv = up(l);
         for (int p = lane; p < parts; p += 32) weight_s[p * QB + qi] = weight(all_s[p * QB + qi]) * inv;
-        if (lane == 0) store_lse(a, c.Hkv, lo, h, c0 + qi, m, l);
+        if (lane == 0) store_lse(a, c.Hkv, lo, h, r0 + qi, m, l);
       }
       __syncthreads();
       for (int x = tid; x < rows * (D / 4); x += NW * 32) {
@@ -565,7 +584,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
 #pragma unroll
           for (int f = 0; f < kFlight; ++f) {
             const int p = min(p0 + f, parts - 1);
-            y[f] = __ldcg(reinterpret_cast<const float4*>(part(c_lo + p, p == 0, pass)) + x);
+            y[f] = __ldcg(reinterpret_cast<const float4*>(part(c_lo + p, p == 0, team)) + x);
           }
 #pragma unroll
           for (int f = 0; f < kFlight; ++f)
@@ -574,7 +593,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
               r.x = fmaf(y[f].x, k, r.x); r.y = fmaf(y[f].y, k, r.y); r.z = fmaf(y[f].z, k, r.z); r.w = fmaf(y[f].w, k, r.w);
             }
         }
-        *reinterpret_cast<float4*>(out_row(a, lo, h, c0 + qi) + x % (D / 4) * 4) = r;
+        *reinterpret_cast<float4*>(out_row(a, lo, h, r0 + qi) + x % (D / 4) * 4) = r;
       }
       __syncthreads();
     }

@@ -129,8 +129,10 @@ size_t attend_scratch(const dkv_cache8* c) {
 
 template <int D, int QB, int kKind>
 cudaError_t set_attend_smem() {
-  const cudaError_t e = cudaFuncSetAttribute(attend8_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(attend8_warps_kernel<D, QB, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
+  cudaError_t e = cudaSuccess;
+  for (auto kernel : {attend8_kernel<D, QB, kKind, false>, attend8_kernel<D, QB, kKind, QB == 16>, attend8_warps_kernel<D, QB, kKind>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_smem<D>());
+  return e;
 }
 template <int D>
 cudaError_t set_attend_smem(int kind) {
@@ -165,7 +167,7 @@ int quad_threads(const dkv_cache8* c) { return c->cfg.page_rows * c->cfg.head_di
 template <int D, int QB, int kKind>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
   const bool warps = attend_by_warps(c, a.n, a.rows);
-  return launch_pdl(warps ? attend8_warps_kernel<D, QB, kKind> : attend8_kernel<D, QB, kKind>, dim3(attend_blocks(c)), kAttendWarps * 32, (size_t)attend_smem<D>(), 1, st, c->view, a);
+  return launch_pdl(warps ? attend8_warps_kernel<D, QB, kKind> : a.slots > 1 ? attend8_kernel<D, QB, kKind, QB == 16> : attend8_kernel<D, QB, kKind, false>, dim3(attend_blocks(c)), kAttendWarps * 32, (size_t)attend_smem<D>(), 1, st, c->view, a);
 }
 template <int D>
 cudaError_t launch_attend(dkv_cache8* c, const AttendArgs& a, cudaStream_t st) {
