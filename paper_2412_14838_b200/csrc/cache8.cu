@@ -71,8 +71,10 @@ bool vectors(const dkv_rows& r) {              // every row starts on a 16-byte 
          (r.tokens == 1 || r.token_stride % per == 0);
 }
 bool valid(const dkv_rotary* r) {
-  return r && r->head_dim >= 2 && r->head_dim <= 256 && r->head_dim % 2 == 0 && r->rot_dim >= 2 && r->rot_dim <= r->head_dim &&
-         r->rot_dim % 2 == 0 && (r->layout == DKV_ROTARY_HALF || r->layout == DKV_ROTARY_PAIRS);
+  if (!r || r->head_dim < 2 || r->head_dim > 256 || r->head_dim % 2 || r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2) return false;
+  double sum = r->amplitude;                   // infinite or NaN where any part of it is
+  for (int i = 0; i < r->rot_dim / 2; ++i) sum += fabs(r->turns[i]);
+  return (r->layout == DKV_ROTARY_HALF || r->layout == DKV_ROTARY_PAIRS) && isfinite(sum);
 }
 
 // ---- rotary positions ---------------------------------------------------------------------------------------------------
@@ -119,9 +121,11 @@ int validate(const dkv_cache8_config* c) {
 constexpr int kMostQueries = 64;               // query rows of a KV head
 
 int attend_blocks(const dkv_cache8* c) { return std::min(c->n_sms, 256); }
-// A slice a warp where there are so many heads that one does not lie in more than some sixteen slices (a single warp merges them)
-// and the query rows fit one pass; else a slice a block.
-bool attend_by_warps(const dkv_cache8* c, int n, int rows) { return rows <= 16 && (long long)n * c->cfg.n_kv_heads * 16 >= attend_blocks(c) * kAttendWarps; }
+// A slice a warp where there are more heads than blocks and the query rows fit one pass; else a slice a block.  Measured, 8 KV heads a
+// sequence, 4 query rows of 128 dims (us, a slice a block / a warp): 8 sequences of 2000 rows 18.4 / 22.6, 16 of 2000 24.3 / 26.5, 16 of
+// 8192 55.1 / 62.1, but 16 of 500 15.3 / 13.9; 32 of 500 22.9 / 18.2, 32 of 2000 38.1 / 37.8, 64 of 2000 60.8 / 57.9.  With few heads a
+// single warp has to merge a great many parts: 1 sequence of 8192 rows 12.2 / 75.9.
+bool attend_by_warps(const dkv_cache8* c, int n, int rows) { return rows <= 16 && (long long)n * c->cfg.n_kv_heads > attend_blocks(c); }
 // Floats of scratch: two parts a slice, of 16 rows a warp or of all a block.
 size_t attend_scratch(const dkv_cache8* c) {
   return (size_t)attend_blocks(c) * 2 * std::max(kAttendWarps * 16, kMostQueries) * (c->cfg.head_dim + 2);

@@ -8,6 +8,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -139,7 +140,10 @@ DKV_PY(get_counts, 3, CTX(0) PTR(o, 1) STREAM(2), dkv_get_counts(c, (int32_t*)o,
 DKV_PY(memcpy_to_host, 5, CTX(0) PTR(dst, 1) PTR(src, 2) SIZE(bytes, 3) STREAM(4), dkv_memcpy_to_host(c, dst, src, bytes, st))
 DKV_PY(kept_sorted, 4, CTX(0) INT(l, 1) PTR(o, 2) STREAM(3), dkv_kept_sorted(c, l, (int32_t*)o, st))
 
-// A strided tensor [batch, heads, tokens, head_dim] on a GPU, None (NULL), or the address of a dkv_rows.  A tensor that has not
+// On the current device, where the calls that take tensors run.
+bool here(const at::Tensor& t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+
+// A strided tensor [batch, heads, tokens, head_dim] on the current GPU, None (NULL), or the address of a dkv_rows.  A tensor that has not
 // this form becomes one without a type, which the library refuses.
 struct Rows {
   dkv_rows own;
@@ -156,7 +160,7 @@ struct Rows {
     own = {};
     own.type = -1;
     p = &own;
-    if (!t.is_cuda() || t.dim() != 4 || (t.size(3) > 1 && t.stride(3) != 1)) return true;
+    if (!here(t) || t.dim() != 4 || (t.size(3) > 1 && t.stride(3) != 1)) return true;
     int32_t size[4];
     for (int i = 0; i < 4; ++i) {
       if (t.size(i) > INT32_MAX) return true;
@@ -175,11 +179,11 @@ struct Rows {
     return true;
   }
 };
-// A contiguous tensor of `need` 32-bit numbers at least on a GPU, None (NULL), or an address.  *bad: it is not that.
+// A contiguous tensor of `need` 32-bit numbers at least on the current GPU, None (NULL), or an address.  *bad: it is not that.
 bool numbers(PyObject* x, c10::ScalarType type, int64_t need, void** out, bool* bad) {
   if (!THPVariable_Check(x)) return address(x, out);
   const at::Tensor& t = THPVariable_Unpack(x);
-  *bad = *bad || !t.is_cuda() || t.scalar_type() != type || !t.is_contiguous() || t.numel() < need;
+  *bad = *bad || !here(t) || t.scalar_type() != type || !t.is_contiguous() || t.numel() < need;
   *out = t.data_ptr();
   return true;
 }

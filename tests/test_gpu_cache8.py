@@ -223,10 +223,11 @@ def test_attention_over_larger_pages(R, kind):
 @pytest.mark.parametrize("G,nq", [(4, 1), (5, 3), (6, 3)])                  # one pass of 8, one of 16, two: another division of the work
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_of_many_heads(kind, io, G, nq, D):
-    lens = [0, 1, 32, 33, 500] + [(i * 97) % 400 for i in range(35)]
-    with Both(n_pages=400, n_seqs=40, max_pages=20, D=D, kind=kind, io=io, G=G, Hkv=3) as c:
-        c.add(0, 40, 1, lens, G)
-        c.attend(0, 40, 1, nq, True)
+    lens = [0, 1, 32, 33, 500] + [(i * 97) % 400 for i in range(55)]
+    with Both(n_pages=600, n_seqs=60, max_pages=20, D=D, kind=kind, io=io, G=G, Hkv=3) as c:
+        c.add(0, 60, 1, lens, G)
+        c.attend(0, 60, 1, nq, True)
+        c.attend(0, 40, 1, nq, True)                                         # fewer heads than blocks
 
 
 def test_a_long_sequence_lies_in_every_block():
@@ -248,7 +249,7 @@ def test_values_at_the_ends_of_bf16(size):
         c.attend(0, 1, 1, 2, False)
 
 
-@pytest.mark.parametrize("n,Hkv", [(1, 2), (60, 2)])                        # a slice a block, a slice a warp
+@pytest.mark.parametrize("n,Hkv", [(1, 2), (60, 3)])                        # a slice a block, a slice a warp
 @pytest.mark.parametrize("chunk", [0, 1])
 def test_a_wait_that_runs_out_is_reported_and_leaves_the_cache_usable(n, Hkv, chunk):
     with Both(n_pages=4000, n_seqs=n, max_pages=900 // n * 4 + 20, Hkv=Hkv) as c:
