@@ -201,6 +201,87 @@ def test_keys_turned_on_the_way_in(layout, rot, D, kind):
             assert (got[1][s, :, :m] == c.o.rows(s, 1)).all()
 
 
+@pytest.mark.parametrize("layout,rot", [("half", 64), ("pairs", 32), ("half", 10), ("pairs", 6)])
+@pytest.mark.parametrize("T", [1, 5, 8, 9])                                  # a block a sequence up to eight rows, then a block a page
+def test_turned_keys_behind_others_and_numbers_that_are_not_finite(layout, rot, T):
+    """As above, behind 30 rows (pages end inside the new ones), with an infinity and a NaN in one new row: what they turn into is NaN
+    or infinite in 64 bits too, and stored as 0 or the largest code."""
+    D = 64
+    freq, amp = C.frequencies(rot, 10000.0)
+    r = B.dkv_rotary_init(D, rot, B.DKV_ROTARY_HALF if layout == "half" else B.DKV_ROTARY_PAIRS, 10000.0)
+    with Both(n_seqs=2, D=D, n_pages=20) as c:
+        c.add(0, 2, 1, [30, 3], 5)
+        k, v = (torch.randn(2, 2, T, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+        k[0, 1, T - 1, 1] = float("nan")
+        k[0, 0, 0, 2] = float("inf")
+        v[1, 0, 0, 3] = float("-inf")
+        v[1, 1, T - 1, 63] = float("nan")
+        pos0 = torch.tensor([77, 0], dtype=torch.int32, device="cuda")
+        B.dkv_cache8_reserve(c.h, 0, 2, 1, None, T)
+        B.dkv_cache8_append(c.h, 0, 2, 1, k, v, None, r, pos0)
+        c.o.reserve([0, 1], [T, T])
+        wants = []
+        for s in range(2):
+            x = k[s].double().cpu().numpy()
+            with np.errstate(invalid="ignore"):
+                wants.append(C.rotate(x, int(pos0[s]) + np.arange(T), freq, amp, layout))
+            c.o.append(s, wants[s], v[s].double().cpu().numpy())
+        got = c.read(0, 2, 1, 30 + T)
+        for s, before in enumerate((30, 3)):
+            assert (got[1][s, :, :before + T] == c.o.rows(s, 1)).all()
+            new, fine = got[0][s, :, before:before + T], np.isfinite(wants[s])
+            scale = c.o.scales(s, 0)[:, before:, None] + 0 * new
+            step = C.step_at(np.where(fine, wants[s], 0), scale, "e4m3")
+            assert (np.abs(new - wants[s])[fine] <= (step / 2 + 2 * 5 * amp * 8e-7)[fine]).all()
+            assert (new[~fine] == c.o.rows(s, 0)[:, before:][~fine]).all()
+            assert (got[0][s, :, :before] == c.o.rows(s, 0)[:, :before]).all()
+        assert B.dkv_cache8_status(c.h)[1][:2] == [B.DKV_C8_NOT_FINITE, 0]
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_many_rows_with_numbers_that_are_not_finite(kind):
+    with Both(n_seqs=2, n_pages=20, kind=kind, D=128) as c:
+        c.add(0, 2, 1, [5, 0], 5)
+        x = torch.randn(2, 2, 70, 128, device="cuda").to(torch.bfloat16)
+        x[0, 0, 3, 7], x[0, 1, 40, 100], x[1, 0, 69, 127], x[1, 1, :, :] = float("nan"), float("-inf"), float("inf"), float("nan")
+        B.dkv_cache8_reserve(c.h, 0, 2, 1, None, 70)
+        B.dkv_cache8_append(c.h, 0, 2, 1, x, x.flip(2))
+        c.o.reserve([0, 1], [70, 70])
+        for s in range(2):
+            c.o.append(s, x[s].double().cpu().numpy(), x[s].flip(1).double().cpu().numpy())
+        c.check()
+        c.attend(0, 2, 1, 1, False)
+        assert B.dkv_cache8_status(c.h)[1][0] == B.DKV_C8_NOT_FINITE
+
+
+def test_two_caches_on_two_streams():
+    with Both(n_pages=60, n_seqs=4, D=128, G=4) as a, Both(n_pages=60, n_seqs=4, D=64, kind="int8", G=2) as b:
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for turn in range(20):
+            for c, s in zip((a, b), streams):
+                with torch.cuda.stream(s):
+                    c.add(0, 4, 1, [turn % 7, 1, 13, 0], turn)
+        torch.cuda.synchronize()
+        for c in (a, b):
+            c.check()
+            c.attend(0, 4, 1, 2, True)
+
+
+def test_forks_between_one_another_s_sequences():
+    with Both(n_pages=30, n_seqs=6) as c:
+        c.add(0, 3, 2, [40, 33, 64], 1)                                      # sequences 0, 2, 4
+        c.add(1, 3, 2, [70, 1, 0], 2)
+        B.dkv_cache8_fork(c.h, 0, 1, 3, 2)                                   # onto 1, 3, 5, whose own pages go back
+        c.o.fork([(0, 1), (2, 3), (4, 5)])
+        c.check()
+        B.dkv_cache8_fork(c.h, 1, 0, 3, 2)                                   # and back: every page is held by both
+        c.o.fork([(1, 0), (3, 2), (5, 4)])
+        c.check()
+        c.add(0, 6, 1, [1, 2, 3, 4, 5, 6], 3, 7.0)
+        c.check()
+
+
 @pytest.mark.parametrize("kind,io", KINDS)
 @pytest.mark.parametrize("G,nq,causal", [(1, 1, False), (4, 1, True), (2, 4, True), (3, 3, False), (4, 4, True), (7, 5, True), (8, 8, True), (17, 1, False)])
 @pytest.mark.parametrize("D", [64, 128])

@@ -2,6 +2,9 @@
 touches a GPU."""
 import ctypes
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -182,3 +185,36 @@ def test_calls_without_a_cache_are_refused():
         assert e.value.code == B.DKV_ERR_INVALID_ARG
     with pytest.raises(TypeError):
         B.dkv_cache8_read(0, 0, 1, 1, "x", rows, 0)
+
+
+def test_a_program_without_torch_makes_the_same_calls():
+    code = """
+import sys
+sys.modules["torch"] = None                                   # "import torch" fails
+from paper_2412_14838_b200 import binding as B
+def refused(call):
+    try: call()
+    except B.DkvError as e: return e.code == B.DKV_ERR_INVALID_ARG
+r = B.dkv_rotary_init(64, 64, B.DKV_ROTARY_PAIRS, 1e4)
+rows = lambda n: B.DkvRows(None, B.DKV_F32, 1, 2, n, 64, 128, 64, 64)
+B.dkv_rotate(r, 0, rows(0), rows(0), stream=0)                # nothing to do
+assert refused(lambda: B.dkv_rotate(r, 4096, rows(3), rows(3), transpose=True, stream=0))      # no data
+assert refused(lambda: B.dkv_cache8_append(0, 0, 1, 1, rows(1), rows(1), None, r, 4096, 0))
+assert refused(lambda: B.dkv_cache8_compact(0, 0, 1, 1, 4096, None, 0, heads=2, cols=3))
+assert refused(lambda: B.dkv_cache8_attend(0, 0, 1, 1, rows(1), rows(1), None, True, 0))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True)
+
+
+@pytest.mark.parametrize("field,value", [("amplitude", math.nan), ("amplitude", math.inf), ("turns", math.nan), ("turns", math.inf)])
+def test_frequencies_that_are_not_finite_are_refused(field, value):
+    r = B.dkv_rotary_init(**GOOD)
+    if field == "turns":
+        r.turns[31] = value
+    else:
+        r.amplitude = value
+    rows = B.DkvRows(4096, B.DKV_F32, 1, 2, 3, 64, 384, 192, 64)
+    with pytest.raises(B.DkvError) as e:
+        B.dkv_rotate(r, 4096, rows, rows, stream=0)
+    assert e.value.code == B.DKV_ERR_INVALID_ARG
