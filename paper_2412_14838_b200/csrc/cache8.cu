@@ -436,15 +436,13 @@ int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, co
   if (heads != c->cfg.n_kv_heads || cols < 0 || (cols && !idx) || !aligned(idx, 4) || !aligned(count, 4)) return DKV_ERR_INVALID_ARG;
   if (n == 0) return DKV_OK;
   const PlanArgs p = {count, c->d_pick, c->d_jobs, c->d_new_table, c->d_new_held, first, step, n, cols};
-  const CompactArgs a = {idx, count, c->d_new_table, c->d_new_held, first, step, cols};
+  const CompactArgs a = {idx, count, c->d_new_table, c->d_new_held, c->d_tickets, first, step, cols};
   cudaStream_t st = as_stream(stream);
   C8_LAUNCH(c, launch_pdl(plan_compact8_kernel, dim3(1), kPlanThreads, 0, 1, st, c->view, p));
-  const int R = c->cfg.page_rows, pages = std::min((int)(((long long)cols + R - 1) / R), c->cfg.max_pages);
-  if (pages)
-    C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto) {
-      return launch_pdl(compact8_kernel<decltype(d)::value, decltype(kind)::value>, dim3(pages, c->cfg.n_kv_heads, n), quad_threads(c), 0, 1, st, c->view, a);
-    }));
-  C8_LAUNCH(c, launch_pdl(install8_kernel, dim3(n), kSeqThreads, 0, 1, st, c->view, a));
+  const int R = c->cfg.page_rows, pages = std::max(1, std::min((int)(((long long)cols + R - 1) / R), c->cfg.max_pages));
+  C8_LAUNCH(c, with_types(c, [&](auto d, auto kind, auto) {
+    return launch_pdl(compact8_kernel<decltype(d)::value, decltype(kind)::value>, dim3(pages, c->cfg.n_kv_heads, n), quad_threads(c), 0, 1, st, c->view, a);
+  }));
   return DKV_OK;
 }
 

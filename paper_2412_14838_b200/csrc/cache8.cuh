@@ -528,7 +528,7 @@ read8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ ReadArgs 
 
 // ---- pages --------------------------------------------------------------------------------------------------------------
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024, kPlanPicks = 4096;       // picks: pages found that shared memory holds
 
 struct PlanArgs {
   const int* count;          // [n] or null: `most` each
@@ -567,9 +567,11 @@ __device__ __forceinline__ long long block_scan(long long v, long long* warp_s, 
 template <bool kCompact>
 __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
   __shared__ long long warp_s[32];
-  __shared__ int jobs_s, prefix_s[kPlanThreads + 1], len_s[kPlanThreads], held_s[kPlanThreads], copies_s[kPlanThreads];
+  __shared__ int jobs_s, prefix_s[kPlanThreads + 1], len_s[kPlanThreads], held_s[kPlanThreads], copies_s[kPlanThreads], pick_s[kPlanPicks];
   const int tid = threadIdx.x;
   if (tid == 0) jobs_s = 0;
+  auto pick = [&](int k) -> int& { return k < kPlanPicks ? pick_s[k] : a.pick[k]; };
+  int hint = __ldcg(c.hint);                                                 // (asked for ahead of its use)
   // Sequences that are served get the pages given out one call after the other, kPlanThreads sequences at a time, as if in one.
   bool lasts = true;
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
@@ -605,26 +607,26 @@ __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
     const int words = (c.n_pages + 31) / 32;
     int found = 0;
     if (all && lasts)
-      for (int w0 = __ldcg(c.hint); w0 < words && found < all; w0 += kPlanThreads) {
+      for (int w0 = hint; w0 < words && found < all; w0 += kPlanThreads) {
         const int w = w0 + tid;
         unsigned int bits = w < words ? __ldcg(c.free + w) : 0;
         long long here;
         int at = found + (int)block_scan(__popc(bits), warp_s, here);
         for (; bits && at < all; bits &= bits - 1) {
-          if (at < c.n_pages) a.pick[at] = w * 32 + __ffs(bits) - 1;
+          if (at < c.n_pages) pick(at) = w * 32 + __ffs(bits) - 1;
           ++at;
         }
         found += (int)here;
       }
     __syncthreads();
     found = min(found, all);
-    if (tid == 0 && all && found == all) *c.hint = a.pick[all - 1] >> 5;
+    if (tid == 0 && all && found == all) *c.hint = pick(all - 1) >> 5;
     __syncthreads();
     for (int k = tid; k < found; k += kPlanThreads) {
       int lo = 0, hi = n - 1;                                                // the last sequence with prefix <= k
       while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (prefix_s[mid] <= k) lo = mid; else hi = mid - 1; }
       if (prefix_s[lo + 1] > found) continue;                                // not served
-      const int s = a.first + (i0 + lo) * a.step, page = a.pick[k], j = k - prefix_s[lo];
+      const int s = a.first + (i0 + lo) * a.step, page = pick(k), j = k - prefix_s[lo];
       if (kCompact) {
         a.new_table[(size_t)s * c.max_pages + j] = page;
       } else {
@@ -651,8 +653,11 @@ __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
       }
     }
     lasts = lasts && found == all;
-    __threadfence();                                                         // the next sequences find `free`, `refs` and the table as they are now
-    __syncthreads();
+    if (i0 + kPlanThreads < a.n) {
+      __threadfence();                                                       // the next sequences find `free`, `refs` and the table as they are now
+      __syncthreads();
+      hint = __ldcg(c.hint);
+    }
   }
   if (!kCompact && tid == 0) a.jobs[0] = jobs_s;
 }
@@ -732,17 +737,20 @@ struct CompactArgs {
   const int* count;          // [n] or null: cols each
   const int* new_table;
   const int* new_held;
+  unsigned int* tickets;     // [n], zero between launches
   int first, step, cols;
 };
 
 // One page and head of a compacted sequence: row j is row idx[j] of the sequence as it is; a new page takes the scales that its rows
 // need.  A quad of keys and one of values a thread, all their loads in flight.  A row's values lie in 32 bytes of every 128, so four
 // times their bytes are read: 28 sequences cut from up to 8K rows to 1000, 4 heads of 128, about 30 us for 66 MB in and 26 out, bound by
-// the latency of its chain of loads (count, row numbers, table, codes).  grid (pages of `cols` rows, Hkv, n).
+// the latency of its chain of loads (count, row numbers, table, codes).  grid (pages of `cols` rows,
+// at least one, Hkv, n).
 template <int D, int kKind>
 __global__ void __launch_bounds__(kQuadThreads, 2)
 compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ CompactArgs a) {
   __shared__ float warp_s[2][kQuadThreads / 32];
+  __shared__ bool last_s;
   const int R = c.R, tid = threadIdx.x, h = blockIdx.y, i = blockIdx.z, seq = a.first + i * a.step;
   const int d = tid % (D / 8) * 8, t = tid / (D / 8) % 4, blk = tid / (D / 2);
   const int* idx = a.idx + ((size_t)i * c.Hkv + h) * a.cols + blockIdx.x * R;
@@ -752,64 +760,64 @@ compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Compac
   int from[4];                                                               // asked for with what says how many count
 #pragma unroll
   for (int k = 0; k < 4; ++k) from[k] = base + quad_row(blk, t, k) < a.cols ? idx[quad_row(blk, t, k)] : -1;
-  const int held = a.new_held[seq], len = c.len[seq], rows = min(R, (a.count ? a.count[i] : a.cols) - base);
-  if ((int)blockIdx.x >= held) return;
-  const int* table = c.table + (size_t)seq * c.max_pages;
-  size_t reg[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const bool wanted = quad_row(blk, t, k) < rows, inside = wanted && from[k] >= 0 && from[k] < len;
-    if (wanted && !inside) report(c, kBadArgument, seq);
-    if (!inside) from[k] = -1;
-    reg[k] = inside ? region(c, table[from[k] >> c.shift], h, 0) : 0;
-  }
-  uint2 key[4];
-  QuadWords value[4];
-  float2 scale[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (from[k] >= 0) {
-      const unsigned char* at = c.pages + reg[k] * (size_t)(R * D);
-      const int r = from[k] & (R - 1);
-      key[k] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
-      value[k] = get_words<D>(at + R * D, r >> 4, (r & 7) >> 1, d, 1, R);
-      scale[k] = *reinterpret_cast<const float2*>(c.scales + reg[k]);
-    }
-  const size_t to = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, 0);
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    Quad x;
-    float most = 0.f;
+  const int held = a.new_held[seq], len = c.len[seq], count = a.count ? a.count[i] : a.cols, rows = min(R, count - base);
+  int* table = c.table + (size_t)seq * c.max_pages;
+  if (held < 0) return;                                                      // the sequence stays as it is
+  if ((int)blockIdx.x < held) {
+    size_t reg[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (from[k] >= 0) {
-        x.row[k] = eight_of<kKind>(which ? row_of_values(value[k], (from[k] & 1) + 2 * (from[k] >> 3 & 1)) : key[k], which ? scale[k].y : scale[k].x);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
+      const bool wanted = quad_row(blk, t, k) < rows, inside = wanted && from[k] >= 0 && from[k] < len;
+      if (wanted && !inside) report(c, kBadArgument, seq);
+      if (!inside) from[k] = -1;
+      reg[k] = inside ? region(c, table[from[k] >> c.shift], h, 0) : 0;
     }
-    const int e = scale_exponent(block_max(most, warp_s[which]), kKind);
-    put_quad<D, kKind>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(-e), which, 0, rows);
-    if (tid == 0) c.scales[to + which] = pow2(e);
+    uint2 key[4];
+    QuadWords value[4];
+    float2 scale[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (from[k] >= 0) {
+        const unsigned char* at = c.pages + reg[k] * (size_t)(R * D);
+        const int r = from[k] & (R - 1);
+        key[k] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
+        value[k] = get_words<D>(at + R * D, r >> 4, (r & 7) >> 1, d, 1, R);
+        scale[k] = *reinterpret_cast<const float2*>(c.scales + reg[k]);
+      }
+    const size_t to = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, 0);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      Quad x;
+      float most = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (from[k] >= 0) {
+          x.row[k] = eight_of<kKind>(which ? row_of_values(value[k], (from[k] & 1) + 2 * (from[k] >> 3 & 1)) : key[k], which ? scale[k].y : scale[k].x);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x.row[k].x[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
+      }
+      const int e = scale_exponent(block_max(most, warp_s[which]), kKind);
+      put_quad<D, kKind>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(-e), which, 0, rows);
+      if (tid == 0) c.scales[to + which] = pow2(e);
+    }
   }
-}
-
-// The compacted sequences take the place of the old ones.  grid (n).
-__global__ void __launch_bounds__(kSeqThreads)
-install8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ CompactArgs a) {
-  const int seq = a.first + blockIdx.x * a.step;
-  pdl_launch();
-  pdl_wait();
-  const int pages = a.new_held[seq];
-  if (pages < 0) return;
-  int* table = c.table + (size_t)seq * c.max_pages;
+  // the last block of the sequence to arrive: nobody needs the old pages any more, the new ones take their place
+  __syncthreads();
+  if (tid == 0) {
+    __threadfence();
+    last_s = atomicAdd(&a.tickets[i], 1u) == gridDim.x * gridDim.y - 1;
+  }
+  __syncthreads();
+  if (!last_s) return;
+  const int* made = a.new_table + (size_t)seq * c.max_pages;
   let_go(c, table, 0, c.held[seq]);
   __syncthreads();
-  for (int j = threadIdx.x; j < pages; j += kSeqThreads) table[j] = a.new_table[(size_t)seq * c.max_pages + j];
-  if (threadIdx.x == 0) { c.held[seq] = pages; c.len[seq] = a.count ? a.count[blockIdx.x] : a.cols; }
+  for (int j = tid; j < held; j += blockDim.x) table[j] = made[j];
+  if (tid == 0) { a.tickets[i] = 0; c.held[seq] = held; c.len[seq] = count; }
 }
 
 }  // namespace dkv
