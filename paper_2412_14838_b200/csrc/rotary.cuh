@@ -3,7 +3,7 @@
 // pairs being dims (i, i + rot_dim/2) or (2i, 2i+1); the gradient is the same with sin negated (A times the inverse turn).
 //
 // Angles are computed in turns (f_i / 2 pi, in 64 bits on the host): position times turns is exact to 2^-53 of its size, its
-// whole part is dropped, and what is left goes to sincospif in 32 bits.  A 32-bit angle would be off by 2^-24 of itself, 0.06
+// whole part is dropped, and what is left goes to sincospif in 32 bits, with a correction.  A 32-bit angle would be off by 2^-24 of itself, 0.06
 // radians at position 10^6.  The pair itself is turned in 32 bits and rounded once.
 #pragma once
 #include <cuda_bf16.h>
@@ -14,10 +14,15 @@
 
 namespace dkv {
 
-// cos and sin of `turns` turns a position.
+// cos and sin of `turns` turns a position.  What the argument loses when it is rounded to 32 bits, up to 2^-25 of a half turn or two
+// steps of the result, is added back to first order.
 __device__ __forceinline__ void turn_of(int pos, double turns, float& c, float& s) {
-  const double x = (double)pos * turns;
-  sincospif((float)(2.0 * (x - rint(x))), &s, &c);
+  const double x = (double)pos * turns, y = 2.0 * (x - rint(x));
+  const float hi = (float)y, lo = 3.14159265f * (float)(y - (double)hi);
+  float c0, s0;
+  sincospif(hi, &s0, &c0);
+  c = fmaf(-lo, s0, c0);
+  s = fmaf(lo, c0, s0);
 }
 
 template <typename T> __device__ __forceinline__ float to_float(T x);

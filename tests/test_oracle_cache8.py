@@ -3,6 +3,7 @@ touches a GPU."""
 import ctypes
 import math
 import os
+import re
 import subprocess
 import sys
 
@@ -218,3 +219,19 @@ def test_frequencies_that_are_not_finite_are_refused(field, value):
     with pytest.raises(B.DkvError) as e:
         B.dkv_rotate(r, 4096, rows, rows, stream=0)
     assert e.value.code == B.DKV_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("header", ["cache8.cuh", "attend8.cuh", "rotary.cuh"])
+def test_every_kernel_waits_for_the_one_before_it_before_it_does_or_skips_anything(header):
+    """All are launched while their predecessor may still run, and each counts on every kernel before it being complete: that
+    holds if no block of any of them ends without its own wait."""
+    from tests.test_launch_overlap import _functions, _source
+    kernels = {n: b for n, _, b in _functions(_source(header)) if n.endswith("_kernel")}
+    assert kernels
+    for name, body in kernels.items():
+        wait = body.index("pdl_wait();")
+        assert body.index("pdl_launch();") < wait, name
+        assert "return" not in body[:wait], name
+        head = body[:wait]
+        assert head.count("{") - head.count("}") == 1, f"{name}: the wait holds for every thread"
+        assert not re.search(r"\bc\.(len|held|table|refs|free|hint|scales|pages)\s*\[", head), f"{name} reads ahead of its wait"
