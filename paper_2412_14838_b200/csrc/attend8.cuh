@@ -3,9 +3,9 @@
 //
 // What must move is every code once, D bytes of keys and D of values a row and head.  There are at most 64 query rows a head, 4
 // or 8 in most models, so both products are warp-wide (mma.sync m16n8k16, fp16 in, fp32 sums): no 128-row tile to give to
-// tcgen05.  Both code types are exact in fp16, and so are the queries once each is scaled by a power of two (8 or 11 bits of a
-// row's largest magnitude down to 2^-24 below the rest's reach); weights are split into two fp16 parts, 22 bits.  The parts
-// lie in the two halves of the 16-row operand where there are at most 8 query rows a head.
+// tcgen05.  Both code types are exact in fp16.  So are the queries, once a power of two has brought a row's largest number to 2^13 and
+// above: what is 2^-17 of it and more keeps its 8 or 11 bits, what is smaller is off by 2^-38 of it.  Weights are split into two
+// fp16 parts, 22 bits, which lie in the two halves of the 16-row operand where there are at most 8 query rows a head.
 //   S = Q K^T   scaled by the page's key scale when it leaves the accumulators;
 //   O = P V     a page's product is added to the result times its value scale.
 // Weights are relative to a reference that a row's largest logit may pass by a factor of 2^7 before it is moved, so that in most steps
@@ -612,9 +612,10 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
 
 // Many heads.  The chunks of all heads form one sequence that is cut into one equal slice a WARP, so that no warp waits for another:
 // no barrier, and the set-up of one warp's head runs beside the other warps' work.  A head counts kAttendHeadCost chunks more
-// than it has.  A head that lies in one slice is finished there; of the others every warp leaves its part in scratch, as it
+// than it has, its set-up and its results: with 1 / 2 / 4 of them 32 sequences of 500 rows, 8 heads of 128, take 18.2 / 16.9 / 16.6 us,
+// 96 of 160 rows 18.8 / 16.3 / 15.8, 64 of 8K the same.  A head that lies in one slice is finished there; of the others every warp leaves its part in scratch, as it
 // lies in its registers, and the warp that arrives last for a head (a ticket) merges the parts in slice order.
-constexpr int kAttendHeadCost = 1;
+constexpr int kAttendHeadCost = 4;
 template <int D, int QB, int kKind>
 __global__ void __launch_bounds__(kAttendWarps * 32, 1)
 attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendArgs a) {
@@ -642,9 +643,8 @@ attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ A
     const int end = min(u1, at.u0 + at.units), first = max(0, u - row0), after = max(0, end - row0);
     u = end;
     if (after == 0 && all > 0) continue;
+    if (all == 0 && own != slices.owner(at.u0 + at.units - 1)) continue;       // a head without rows is its last unit's
     const bool whole = first == 0 && after == all;
-    const int c_lo = slices.owner(all > 0 ? row0 : at.u0), c_hi = slices.owner(at.u0 + at.units - 1);
-    if (all == 0 && own != c_hi) continue;             // (a head without rows whose cost is several units)
     Warp w;
     typename Warp::Raw raw;
     Warp::ask(raw, a, at.i, at.h, 0, g, t);
@@ -652,6 +652,7 @@ attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ A
     if (ring.broken && lane == 0) report(c, kTimeout, seq);
     w.add_up();
     if (whole) { w.store(a, c.Hkv, at.i, at.h, g, t); continue; }
+    const int c_lo = slices.owner(row0), c_hi = slices.owner(at.u0 + at.units - 1);
     auto part = [&](int sl, bool first) { return a.scratch + (size_t)(2 * sl + first) * (QB * (D + 2)); };
     w.save(part(own, first == 0), lane, g, t);
     unsigned int* ticket = a.tickets + (size_t)at.i * c.Hkv + at.h;
