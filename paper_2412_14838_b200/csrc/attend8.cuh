@@ -277,7 +277,7 @@ struct AttendWarp {
   // The saved results part(0), part(1), .. added up in that order.
   template <typename F>
   __device__ __forceinline__ void merge(F part, int parts, int lane, int g) {
-    constexpr int kFlight = 256 / D;                 // parts whose loads are in flight together, as many as the registers take
+    constexpr int kFlight = D == 64 ? 6 : 2;         // parts whose loads are in flight together, as many as the registers take
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       float m = -INFINITY, l = 0.f;
