@@ -364,7 +364,7 @@ int dkv_rotary_init(const dkv_rotary_config* cfg, dkv_rotary* out);
 /* Turn x into x_out, and y into y_out where y is given (queries and keys of one call; same batch, tokens, head_dim and type).
  *   pos : int32 [batch][tokens], device: positions, of any size or sign.  Angles are reduced in 64 bits.
  *   transpose != 0: the gradient, i.e. sin negated: given d/d x_out it writes d/d x.
- * fp32 arithmetic, one rounding.  x_out may be x itself (same strides); no other overlap, and no element of an output twice.
+ * fp32 arithmetic, one rounding.  At most 65535 heads in x and y together.  x_out may be x itself (same strides); no other overlap, and no element of an output twice.
  * Errors: INVALID_ARG (also a type DKV_RAW16, or data not aligned to its element).  The call may be captured into a CUDA graph. */
 int dkv_rotate(const dkv_rotary* r, const int32_t* pos, const dkv_rows* x, const dkv_rows* x_out, const dkv_rows* y,
                const dkv_rows* y_out, int32_t transpose, void* stream);

@@ -408,11 +408,6 @@ DKV_E4M3, DKV_INT8 = 0, 1
 DKV_C8_NO_PAGES, DKV_C8_TABLE_FULL, DKV_C8_NO_ROOM, DKV_C8_BAD_ARGUMENT, DKV_C8_NOT_FINITE, DKV_C8_TIMEOUT = 1, 2, 4, 8, 16, 32
 
 
-def _struct(x):
-    """The address of a structure; anything else as it is."""
-    return ctypes.addressof(x) if isinstance(x, ctypes.Structure) else x
-
-
 def dkv_rotary_init(head_dim: int, rot_dim: int, layout: int, theta: float, scaling: int = DKV_SCALING_NONE, factor: float = 1.0,
                     low: float = 1.0, high: float = 4.0, trained_len: float = 8192.0) -> DkvRotary:
     """Frequencies of rotary positions, for dkv_rotate and dkv_cache8_append."""
@@ -423,7 +418,7 @@ def dkv_rotary_init(head_dim: int, rot_dim: int, layout: int, theta: float, scal
 
 def dkv_rotate(rotary: DkvRotary, pos, x, x_out, y=None, y_out=None, transpose=False, stream=None) -> None:
     """Turn x [batch, heads, tokens, head_dim] by the positions int32 [batch, tokens], and y with it; transpose: the gradient."""
-    _check(_native().rotate(_struct(rotary), pos, _struct(x), _struct(x_out), _struct(y), _struct(y_out), transpose, stream), "dkv_rotate")
+    _check(_native().rotate(rotary, pos, x, x_out, y, y_out, transpose, stream), "dkv_rotate")
 
 
 def make_cache8_config(n_pages, page_rows, n_seqs, max_pages, n_q_heads, n_kv_heads, head_dim, kind=DKV_E4M3, io=DKV_BF16) -> DkvCache8Config:
@@ -448,17 +443,17 @@ def dkv_cache8_reserve(cache: int, first: int, n: int, step: int, rows=None, add
 def dkv_cache8_append(cache: int, first: int, n: int, step: int, k, v, rows=None, rotary: Optional[DkvRotary] = None, pos0=None,
                       stream=None) -> None:
     """Add the first rows[i] rows of k[i], v[i] [n, n_kv_heads, tokens, head_dim], the keys turned from position pos0[i] on."""
-    _check(_native().cache8_append(cache, first, n, step, _struct(k), _struct(v), rows, _struct(rotary), pos0, stream), "dkv_cache8_append")
+    _check(_native().cache8_append(cache, first, n, step, k, v, rows, rotary, pos0, stream), "dkv_cache8_append")
 
 
 def dkv_cache8_read(cache: int, first: int, n: int, step: int, k_out, v_out, stream=None) -> None:
     """The sequences' rows as 16-bit numbers into k_out, v_out [n, n_kv_heads, tokens, head_dim]."""
-    _check(_native().cache8_read(cache, first, n, step, _struct(k_out), _struct(v_out), stream), "dkv_cache8_read")
+    _check(_native().cache8_read(cache, first, n, step, k_out, v_out, stream), "dkv_cache8_read")
 
 
 def dkv_cache8_attend(cache: int, first: int, n: int, step: int, q, out, lse=None, causal=False, stream=None) -> None:
     """Attention of q [n, n_q_heads, nq, head_dim] over the sequences' rows into out (fp32) and lse (fp32 [n, n_q_heads, nq])."""
-    _check(_native().cache8_attend(cache, first, n, step, _struct(q), _struct(out), lse, causal, stream), "dkv_cache8_attend")
+    _check(_native().cache8_attend(cache, first, n, step, q, out, lse, causal, stream), "dkv_cache8_attend")
 
 
 def dkv_cache8_fork(cache: int, src: int, dst: int, n: int, step: int, stream=None) -> None:

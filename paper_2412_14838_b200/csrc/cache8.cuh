@@ -663,7 +663,8 @@ __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
 }
 
 // A cluster of kPlanBlocks: its first block plans, then all of them copy the pages that sequences shared and are to write to
-// (jobs[1 + 2 j] to jobs[2 + 2 j], all heads), mostly none: a launch of its own for that cost every step 2.4 us more.
+// (jobs[1 + 2 j] to jobs[2 + 2 j], all heads), mostly none: a launch of its own for that cost every step 2 us more (32 sequences 4.9
+// us, now 3.5).
 constexpr int kPlanBlocks = 8;
 __global__ void __launch_bounds__(kPlanThreads)
 reserve8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ PlanArgs a) {

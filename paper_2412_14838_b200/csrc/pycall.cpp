@@ -22,11 +22,18 @@ namespace {
 
 constexpr Py_ssize_t kMaxList = 4096;       // longest list of per-layer tensors taken
 
-// Address of a torch tensor, an integer, None (NULL), or of anything with data_ptr() (a tensor subclass may have its own)
+// Address of a torch tensor, a ctypes structure, an integer, None (NULL), or of anything with data_ptr() (a tensor subclass may have its own)
 // or a numpy-like .ctypes.data.
 bool address(PyObject* x, void** out) {
   if (x == Py_None) { *out = nullptr; return true; }
   if (THPVariable_CheckExact(x)) { *out = THPVariable_Unpack(x).data_ptr(); return true; }
+  if (PyObject_CheckBuffer(x) && PyObject_HasAttrString(x, "_fields_")) {       // a ctypes structure: its own memory
+    Py_buffer b;
+    if (PyObject_GetBuffer(x, &b, PyBUF_SIMPLE) < 0) return false;
+    *out = b.buf;
+    PyBuffer_Release(&b);
+    return true;
+  }
   PyObject* v = nullptr;
   if (PyLong_Check(x)) {
     v = x;
