@@ -32,11 +32,15 @@ __device__ __forceinline__ float fast_exp2(float x) {
 //   rb_collect_kernel              scores                  rb_locate_kernel
 //   select_gather_kernel,          scores                  rb_finish_kernel
 //   select_gather_cluster_kernel
-// (decode_cluster_kernel only asks for lines to be brought to L2.)  Such memory is not read-only for the lifetime of the grid: a
+// (decode_cluster_kernel and the attend8 kernels only ask for lines to be brought to L2.)  Such memory is not read-only for the lifetime of the grid: a
 // kernel with pdl_wait takes its pointers without __restrict__ and reads with plain loads (no __ldg), which the compiler may
 // neither turn into non-coherent loads nor move above the wait.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Asks for a 128-byte line to be brought to L2.  Nothing is read: a write that comes later finds its line there, so this may
+// stand before pdl_wait.
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Per-layer device pointers passed by value to kernels that work on several layers at once.
 struct LayerPtrs {

@@ -52,10 +52,6 @@ __device__ __forceinline__ uint32_t pack_hi(float a, float b) { return __byte_pe
 __device__ __forceinline__ float rest_of(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
 __device__ __forceinline__ uint4 ld_row16(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 
-// Asks for a 128-byte line to be brought to L2.  Nothing is read: a write that comes later finds its line there, so this may
-// stand before pdl_wait.
-__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
 // State of one warp: QB (8 or 16) queries against the rows it has seen.  Lane (g, t) = (lane / 4, lane % 4) holds
 // queries g (and g + 8), output dims 64*(j/8) + 16 t + {j%8, 8 + j%8}, j < D/8.
 template <int D, int QB>

@@ -80,7 +80,8 @@ __device__ __forceinline__ void set_two(Pack<T, V>& p, int i, float2 v) {
 // A block has a few tokens and all heads: it computes every (token, pair)'s cosine and sine once, into shared memory; then a thread
 // has one piece of a token (V pairs, or 2 V dims that only move), keeps its cosines and sines in registers and turns the piece
 // in every groups-th head, kRotateFlight heads' loads in flight.  Bound by HBM where there is much to do, by latency where there is
-// one token.  (With cosines computed by every thread for sixteen heads a 32K prompt of 40 heads took 179 us.)
+// one token.  A 32K prompt of 40 heads of 128 dims in bf16: 671 MB in 114 us, 5.9 TB/s (with cosines computed by every thread for
+// sixteen heads 179).
 constexpr int kRotateThreads = 256, kRotateFlight = 4, kRotateTokens = 16;
 template <typename T, int V, bool kPairs>
 __global__ void __launch_bounds__(kRotateThreads, 3)
