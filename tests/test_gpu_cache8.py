@@ -681,3 +681,13 @@ def test_a_prompt_s_way_into_pages_and_through_decoding(kind):
             c.o.trim(l * w.Bt + 1, 0)
         c.check()
         assert B.dkv_cache8_status(c.h)[1][:3] == [0, -1, sum(x == 0 for x in c.o.refs())]
+
+
+def test_a_cache_that_does_not_fit_is_refused_and_nothing_is_kept():
+    free = torch.cuda.mem_get_info()[0]
+    with pytest.raises(B.DkvError) as e:
+        B.dkv_cache8_create(B.make_cache8_config(2**26, 128, 1, 1, 8, 8, 128))       # 17 TB
+    assert e.value.code == B.DKV_ERR_NOMEM and torch.cuda.mem_get_info()[0] == free
+    with Both() as c:                                                        # the failure is not taken for a later call's
+        c.add(0, 2, 1, [3, 40], 1)
+        c.check()
