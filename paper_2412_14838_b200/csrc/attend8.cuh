@@ -22,6 +22,7 @@
 #pragma once
 #include "cache8.cuh"
 #include "merge.cuh"
+#include "ring.cuh"
 
 namespace dkv {
 
@@ -364,9 +365,8 @@ struct Ring {
   unsigned char* at;
   uint32_t at_s, bar_s;
   long long limit;
-  int stage = 0, phase = 0;                            // of the next chunk that is waited for
+  RingPlaces<kAttendStages> places;
   int withhold;
-  bool broken = false;                                 // a wait ran out: nothing more is asked for or waited for
 
   __device__ __forceinline__ void start(unsigned char* ring, unsigned long long* bars, int lane, const AttendArgs& a) {
     at = ring; limit = a.wait;
@@ -378,18 +378,14 @@ struct Ring {
     }
     __syncwarp();
   }
-  // What is still on its way ends before the block does.
-  __device__ __forceinline__ void finish() {
-    if (broken)
-      for (int i = 0; i < kAttendStages; ++i) ring_wait(bar_s + i * 8, i < stage ? phase ^ 1 : phase, limit);
-  }
-  // Adds `count` chunks of head h to w: chunk x is rows first + 32 step x and on.
+  __device__ __forceinline__ bool broken() const { return places.broken; }
+  // Adds `count` chunks of head h to w: chunk x is rows first + 32 step x and on.  No copy is on its way when this returns.
   template <int QB, int kKind>
   __device__ __forceinline__ void run(AttendWarp<D, QB, kKind>& w, const typename AttendWarp<D, QB, kKind>::Raw& raw, const Cache8& c, const AttendArgs& a,
                                       const int* table, int h, int c0, int len, int first, int step, int count, int lane, int g, int t) {
     // page and scales of the next 32 chunks, one a lane
     int page = 0;
-    float2 sc = make_float2(0.f, 0.f);
+    float2 sc = make_float2(0.f, 0.f), now = sc;       // `now`: of the chunks being worked on (`sc` runs ahead)
     auto look = [&](int x0) {
       const int x = x0 + lane;
       if (x < count) {
@@ -397,34 +393,32 @@ struct Ring {
         sc = *reinterpret_cast<const float2*>(c.scales + region(c, page, h, 0));
       }
     };
-    auto fetch = [&](int x, int into) {                // chunk x on its way into its place of the ring
-      if (x >= count || broken) return;
+    auto ask = [&](int x, int into) {                  // chunk x on its way into its place of the ring
+      if (x && (x & 31) == 0) look(x);
       const int row = first + x * step * kAttendRows, p = __shfl_sync(0xFFFFFFFFu, page, x & 31);
+      const bool withheld = withhold >= 0 && withhold-- == 0;
+      __syncwarp();                                    // every lane is done with the place
       if (lane == 0) {
         const unsigned char* k = c.pages + region(c, p, h, 0) * (size_t)(c.R * D) + (row & (c.R - 1)) * D;
         const uint32_t bar = bar_s + into * 8, to = at_s + into * kChunkBytes;
         ring_expect(bar, kChunkBytes);
-        if (withhold-- == 0) return;
-        if (c.R == kAttendRows) ring_copy(to, k, kChunkBytes, bar);
-        else { ring_copy(to, k, kHalfBytes, bar); ring_copy(to + kHalfBytes, k + c.R * D, kHalfBytes, bar); }
+        if (!withheld) {
+          if (c.R == kAttendRows) ring_copy(to, k, kChunkBytes, bar);
+          else { ring_copy(to, k, kHalfBytes, bar); ring_copy(to + kHalfBytes, k + c.R * D, kHalfBytes, bar); }
+        }
       }
+      return !withheld;
     };
-    look(0);
-#pragma unroll
-    for (int x = 0; x < kAttendStages - 1; ++x) fetch(x, (stage + x) % kAttendStages);
-    w.start(raw, a, c0, len, g);
-    float2 now = sc;                                   // scales of the chunks being worked on (`sc` runs ahead)
-    for (int x = 0; x < count; ++x) {
+    auto wait = [&](int place, int parity) { return __all_sync(0xFFFFFFFFu, ring_wait(bar_s + place * 8, parity, limit)) != 0; };
+    auto use = [&](int x, int place) {
       if ((x & 31) == 0) now = sc;
-      if (((x + kAttendStages - 1) & 31) == 0) look(x + kAttendStages - 1);
-      __syncwarp();                                    // every lane is done with the place that is filled next
-      fetch(x + kAttendStages - 1, (stage + kAttendStages - 1) % kAttendStages);
-      if (!broken) broken = !__all_sync(0xFFFFFFFFu, ring_wait(bar_s + stage * 8, phase, limit));
       const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = kDown * __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
-      const unsigned char* k = at + stage * kChunkBytes;
-      if (!broken) w.add(reinterpret_cast<const uint4*>(k), reinterpret_cast<const uint4*>(k + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, first + x * step * kAttendRows, lane, t);
-      if (++stage == kAttendStages) { stage = 0; phase ^= 1; }
-    }
+      const unsigned char* k = at + place * kChunkBytes;
+      w.add(reinterpret_cast<const uint4*>(k), reinterpret_cast<const uint4*>(k + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, first + x * step * kAttendRows, lane, t);
+    };
+    static_assert(kAttendStages <= 32);                // chunk 32 i is used before the scales of chunk 32 (i + 1) are looked up
+    look(0);
+    places.run(count, ask, [&] { w.start(raw, a, c0, len, g); }, wait, use);
   }
 };
 
@@ -535,7 +529,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
       const int mine = max(0, (ch1 - ch0 - member + size - 1) / size);       // this warp's chunks: ch0 + member + size x
       Warp::ask(raw, a, lo, h, c0, g, t);
       ring.run(w, raw, c, a, c.table + (size_t)seq * c.max_pages, h, c0, len, (ch0 + member) * kAttendRows, size, mine, lane, g, t);
-      if (ring.broken && lane == 0) report(c, kTimeout, seq);
+      if (ring.broken() && lane == 0) report(c, kTimeout, seq);
       __syncthreads();
       w.add_up();
       w.park(part_s + warp * QB * (D + 4), ml_s + warp * QB, g, t);
@@ -615,7 +609,6 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
   }
-  ring.finish();
 }
 
 // Many heads.  The chunks of all heads form one sequence that is cut into one equal slice a WARP, so that no warp waits for another:
@@ -658,7 +651,7 @@ attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ A
     typename Warp::Raw raw;
     Warp::ask(raw, a, at.i, at.h, 0, g, t);
     ring.run(w, raw, c, a, c.table + (size_t)seq * c.max_pages, at.h, 0, len, first * kAttendRows, 1, after - first, lane, g, t);
-    if (ring.broken && lane == 0) report(c, kTimeout, seq);
+    if (ring.broken() && lane == 0) report(c, kTimeout, seq);
     w.add_up();
     if (whole) { w.store(a, c.Hkv, at.i, at.h, g, t); continue; }
     const int c_lo = slices.owner(row0), c_hi = slices.owner(at.u0 + at.units - 1);
@@ -675,7 +668,6 @@ attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ A
     w.store(a, c.Hkv, at.i, at.h, g, t);
     if (lane == 0) *ticket = 0;
   }
-  ring.finish();
 }
 
 }  // namespace dkv
