@@ -386,19 +386,26 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
         for (int k = 0; k < 4; ++k) odd |= settle(x.row[k], most);
         if (odd) report(c, kNotFinite, seq);
       }
-      int e = scale_exponent(block_max(most, warp_s[y & 1]), kKind);
+      int e = scale_exponent(block_max(most, warp_s[y & 1]), kKind), grown = 0;
       if (r0) {
-        const float old = c.scales[reg];
-        e = max(e, exponent_of(old));
-        const Quad w = quad_of<kKind>(get_words<D>(to, blk, t, d, which, r0), old, which);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) if (quad_row(blk, t, k) < r0) x.row[k] = w.row[k];
-        __syncthreads();                                                     // the whole block has read the old scale
+        const int old = exponent_of(c.scales[reg]);
+        grown = max(0, e - old);
+        e = max(e, old);
       }
       if (odd)
 #pragma unroll
         for (int k = 0; k < 4; ++k) cut<kKind>(x.row[k], pow2(e));
-      put_quad<D, kKind>(to, blk, t, d, x, pow2(-e), which, 0, r1);
+      float inv = pow2(-e);
+      if (r0) {                                                              // all rows in units of the new scale: an old value may be beyond fp32
+        const Quad w = quad_of<kKind>(get_words<D>(to, blk, t, d, which, r0), pow2(max(-126, -grown)), which);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x.row[k].x[i] = quad_row(blk, t, k) < r0 ? w.row[k].x[i] : x.row[k].x[i] * inv;
+        inv = 1.f;
+        __syncthreads();                                                     // the whole block has read the old scale
+      }
+      put_quad<D, kKind>(to, blk, t, d, x, inv, which, 0, r1);
       if (tid == 0) c.scales[reg] = pow2(e);
     }
   }
