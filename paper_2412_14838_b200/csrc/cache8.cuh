@@ -47,12 +47,12 @@ __device__ __forceinline__ size_t region(const Cache8& c, int page, int h, int w
 // Place of a key's code within its region: row r, dim d.
 template <int D>
 __device__ __forceinline__ int key_at(int r, int d) { return (r >> 4) * 16 * D + ((r >> 3) & 1) * 8 * D + (d >> 6) * 512 + (r & 7) * 64 + (d & 63); }
-// Exponent of the smallest power of two s >= 2^-126 with most <= largest code * s; most is finite and not negative.
-// 448 = 0x1.Cp8, 127 = 0x1.FCp6.
-__device__ __forceinline__ int scale_exponent(float most, int kind) {
+// Exponent, at least `low`, of the smallest power of two s with most <= largest code * s; most is finite and not negative, and subnormal
+// only where `low` is above all that it could give (-132).  448 = 0x1.Cp8, 127 = 0x1.FCp6.
+__device__ __forceinline__ int scale_exponent(float most, int kind, int low = -126) {
   const unsigned int b = __float_as_uint(most);
   const int e = (int)(b >> 23) - 127, m = (int)(b & 0x7FFFFFu);
-  return max(-126, kind == kE4m3 ? e - 8 + (m > 0x600000) : e - 6 + (m > 0x7E0000));
+  return max(low, kind == kE4m3 ? e - 8 + (m > 0x600000) : e - 6 + (m > 0x7E0000));
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned int)(e + 127) << 23); }       // -126 <= e <= 127
 __device__ __forceinline__ int exponent_of(float s) { return (int)(__float_as_uint(s) >> 23) - 127; }          // of a power of two
@@ -791,6 +791,7 @@ compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Compac
         key[k] = *reinterpret_cast<const uint2*>(at + key_at<D>(r, d));
         value[k] = get_words<D>(at + R * D, r >> 4, (r & 7) >> 1, d, 1, R);
         scale[k] = *reinterpret_cast<const float2*>(c.scales + reg[k]);
+        scale[k].x *= 0.0625f; scale[k].y *= 0.0625f;                        // the largest values, 448 * 2^120, pass fp32; the smallest, 2^-139 now, do not
       }
     const size_t to = region(c, a.new_table[(size_t)seq * c.max_pages + blockIdx.x], h, 0);
 #pragma unroll
@@ -808,8 +809,13 @@ compact8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ Compac
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x.row[k].x[e]));
       }
-      const int e = scale_exponent(block_max(most, warp_s[which]), kKind);
-      put_quad<D, kKind>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(-e), which, 0, rows);
+      const int e = scale_exponent(block_max(most, warp_s[which]), kKind, -130) + 4;
+      if (e < -123)                                                          // 2^(4-e) would pass fp32
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x.row[k].x[i] *= 8.f;
+      put_quad<D, kKind>(c.pages + (to + which) * (size_t)(R * D), blk, t, d, x, pow2(e < -123 ? 1 - e : 4 - e), which, 0, rows);
       if (tid == 0) c.scales[to + which] = pow2(e);
     }
   }

@@ -48,3 +48,27 @@ def test_the_largest_numbers_stay_what_they_are_behind_other_rows(kind, held, mo
         put(c, 0, 2, y, y)
         c.check()
         c.attend(0, 2, 1, 1, False, scale=0.0)                               # q = 0: the average of all rows
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_the_largest_numbers_stay_what_they_are_in_a_compaction(kind):
+    with Both(kind=kind, n_seqs=2, D=128) as c:
+        x = signs(2, 2, 40, 128, BIG)
+        x[1, :, 7:30] = 2.0 ** -100                                          # a page whose values are far apart
+        put(c, 0, 2, x, -x)
+        idx = [np.stack([np.arange(39, 2, -1), np.arange(37)]) for _ in range(2)]
+        B.dkv_cache8_compact(c.h, 0, 2, 1, torch.tensor(np.stack(idx), dtype=torch.int32, device="cuda"))
+        c.o.compact([0, 1], [i.tolist() for i in idx])
+        c.check()
+        c.attend(0, 2, 1, 1, False, scale=0.0)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -121, 2.0 ** -127, 2.0 ** -133])
+def test_the_smallest_numbers_in_a_compaction(size):
+    with Both(n_seqs=1) as c:
+        x = (torch.randint(-64, 65, (1, 2, 50, 64), device="cuda") * (size / 64 if size > 2.0 ** -127 else size)).to(torch.bfloat16)
+        put(c, 0, 1, x, x.flip(2))
+        idx = np.stack([np.arange(49, 9, -1), np.arange(40)])
+        B.dkv_cache8_compact(c.h, 0, 1, 1, torch.tensor(idx[None], dtype=torch.int32, device="cuda"))
+        c.o.compact([0], [idx.tolist()])
+        c.check()
