@@ -278,23 +278,23 @@ __device__ __forceinline__ float2 turned_by(const AppendArgs& a, int pos, int pa
   turn_of(pos, a.turns[pair], c, s);
   return make_float2(a.amplitude * c, a.amplitude * s);
 }
-// The largest finite magnitude of eight numbers; NaN becomes 0 and what is infinite the largest float.  Whether there were some.
+// The largest finite magnitude of eight numbers; NaN becomes 0.  Whether there were some that are not finite.
 __device__ __forceinline__ bool settle(Eight& x, float& most) {
   bool odd = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float m = fabsf(x.x[e]);
     if (m < INFINITY) most = fmaxf(most, m);
-    else { odd = true; x.x[e] = m == INFINITY ? copysignf(3.402823466e38f, x.x[e]) : 0.f; }
+    else { odd = true; if (m != INFINITY) x.x[e] = 0.f; }
   }
   return odd;
 }
-// Numbers that settle() changed, cut to the largest code once the scale is known.
+// Settled numbers times inv, which brings all finite ones within the codes: what is infinite becomes the largest.
 template <int kKind>
-__device__ __forceinline__ void cut(Eight& x, float scale) {
-  const float most = (kKind == kE4m3 ? 448.f : 127.f) * scale;
+__device__ __forceinline__ void cut(Eight& x, float inv) {
+  constexpr float most = kKind == kE4m3 ? 448.f : 127.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x.x[e] = fminf(fmaxf(x.x[e], -most), most);
+  for (int e = 0; e < 8; ++e) x.x[e] = fminf(fmaxf(x.x[e] * inv, -most), most);
 }
 // Whether `add` rows go behind the `len` rows of a sequence; if not, why (a status bit), else 0.
 __device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, const int* table, int len, int held, int add) {
@@ -392,10 +392,12 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
         grown = max(0, e - old);
         e = max(e, old);
       }
-      if (odd)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) cut<kKind>(x.row[k], pow2(e));
       float inv = pow2(-e);
+      if (odd) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) cut<kKind>(x.row[k], inv);
+        inv = 1.f;
+      }
       if (r0) {                                                              // all rows in units of the new scale: an old value may be beyond fp32
         const Quad w = quad_of<kKind>(get_words<D>(to, blk, t, d, which, r0), pow2(max(-126, -grown)), which);
 #pragma unroll
@@ -492,8 +494,8 @@ append8_few_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ App
       for (int p = 0; p < kPer; ++p) {
         const int j = (lane + 32 * p) / (D / 8), d = (lane + 32 * p) % (D / 8) * 8, r = len + j - base;
         if (j < add && r >= r0 && r < r1) {
-          cut<kKind>(x[p], pow2(e));
-          put_row<D, kKind>(to, r, d, x[p], inv, which);
+          cut<kKind>(x[p], inv);
+          put_row<D, kKind>(to, r, d, x[p], 1.f, which);
         }
       }
       __syncwarp();                                                          // every lane has read the old scale

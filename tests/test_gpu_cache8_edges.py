@@ -72,3 +72,22 @@ def test_the_smallest_numbers_in_a_compaction(size):
         B.dkv_cache8_compact(c.h, 0, 1, 1, torch.tensor(idx[None], dtype=torch.int32, device="cuda"))
         c.o.compact([0], [idx.tolist()])
         c.check()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("rows", [4, 20])
+def test_infinities_are_the_largest_code_of_a_page_of_the_largest_numbers(kind, rows):
+    """448 * 2^120 or 127 * 2^122: seen by attention, whose average of one such row among many is an fp32 number."""
+    with Both(kind=kind, n_seqs=1) as c:
+        y = torch.ones(1, 2, 28, 64, device="cuda").to(torch.bfloat16)
+        put(c, 0, 1, y, y)
+        x = signs(1, 2, rows, 64, BIG)
+        x[0, 0, 0, 0], x[0, 1, 2, 6], x[0, 0, 1, 3] = float("inf"), float("-inf"), float("nan")
+        put(c, 0, 1, x, x)
+        c.attend(0, 1, 1, 1, False, scale=0.0)
+        put(c, 0, 1, y[:, :, :9], y[:, :, :9])                               # rounded again
+        c.attend(0, 1, 1, 1, False, scale=0.0)
+        idx = np.stack([np.arange(c.o.len[0])] * 2)
+        B.dkv_cache8_compact(c.h, 0, 1, 1, torch.tensor(idx[None], dtype=torch.int32, device="cuda"))
+        c.o.compact([0], [idx.tolist()])
+        c.attend(0, 1, 1, 1, False, scale=0.0)
