@@ -371,7 +371,7 @@ append8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AppendA
         if (turned && is_new(k)) turn_row<kIo>(x.row[k], bits, a, from_k + (y >> 1) * head_k + quad_row(blk, t, k) * token_k, d, [&](int pair) { return turn_s[quad_row(blk, t, k) * (a.rot / 2) + pair]; });
       }
       float most = largest_of<kIo>(bits);
-      bool odd = has_odd<kIo>(bits) || (turned && !(most * a.amplitude < 1e38f));       // turned numbers are at most twice as large: finite
+      bool odd = has_odd<kIo>(bits) || (turned && !(most * fabsf(a.amplitude) < 1e38f));       // turned numbers are at most twice as large: finite
       if (turned && !odd) {
         most = 0.f;
 #pragma unroll

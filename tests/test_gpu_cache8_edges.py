@@ -91,3 +91,30 @@ def test_infinities_are_the_largest_code_of_a_page_of_the_largest_numbers(kind, 
         B.dkv_cache8_compact(c.h, 0, 1, 1, torch.tensor(idx[None], dtype=torch.int32, device="cuda"))
         c.o.compact([0], [idx.tolist()])
         c.attend(0, 1, 1, 1, False, scale=0.0)
+
+
+@pytest.mark.parametrize("layout,rot", [("half", 64), ("pairs", 32), ("half", 10)])
+@pytest.mark.parametrize("T", [5, 20])
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_a_negative_amplitude_turns_keys_into_the_negatives_of_a_positive_one_s(layout, rot, T, kind):
+    """dkv_rotary is plain data of the caller's: near the largest numbers the products pass fp32's range, with either sign."""
+    r = [B.dkv_rotary_init(64, rot, B.DKV_ROTARY_HALF if layout == "half" else B.DKV_ROTARY_PAIRS, 10000.0) for _ in range(2)]
+    r[0].amplitude, r[1].amplitude = 3.0, -3.0
+    with Both(n_seqs=2, oracle=False, kind=kind) as c:
+        k = torch.randn(1, 2, T, 64, device="cuda")
+        k[:, 0, T // 2:] *= 1e38
+        k[:, 1, 0, 3] = 3e38
+        k = k.to(torch.bfloat16)
+        k[..., rot:] = 0.0
+        pos0 = torch.tensor([100], dtype=torch.int32, device="cuda")
+        B.dkv_cache8_reserve(c.h, 0, 2, 1, None, T)
+        found = []
+        for s in range(2):
+            B.dkv_cache8_append(c.h, s, 1, 1, k, torch.zeros_like(k), None, r[s], pos0)
+            found.append(B.dkv_cache8_status(c.h)[1][0])
+        got = c.read(0, 2, 1, T)[0]
+        assert np.isfinite(got).all() and (got[0] == -got[1]).all()
+        assert found[0] == found[1]
+        q, out = torch.randn(2, 4, 1, 64, device="cuda").to(torch.bfloat16) * 0, torch.zeros(2, 4, 1, 64, device="cuda")
+        B.dkv_cache8_attend(c.h, 0, 2, 1, q, out)
+        assert (out == 0).all()                                              # logits of 0 * key: NaN were a key NaN or infinite
