@@ -644,7 +644,6 @@ __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
           const int at = len_s[lo] >> c.shift, old = table[at], job = atomicAdd(&jobs_s, 1);
           a.jobs[1 + 2 * job] = old; a.jobs[2 + 2 * job] = page;
           table[at] = page;
-          if (atomicSub(&c.refs[old], 1) == 1) { atomicOr(&c.free[old >> 5], 1u << (old & 31)); atomicMin(c.hint, old >> 5); }
         } else {
           table[held_s[lo] + j - copies_s[lo]] = page;
         }
@@ -663,12 +662,18 @@ __device__ __forceinline__ void plan_pages(const Cache8& c, const PlanArgs& a) {
     }
     lasts = lasts && found == all;
     if (i0 + kPlanThreads < a.n) {
-      __threadfence();                                                       // the next sequences find `free`, `refs` and the table as they are now
+      __threadfence();                                                       // the next sequences find `free` and the table as they are now
       __syncthreads();
       hint = __ldcg(c.hint);
     }
   }
-  if (!kCompact && tid == 0) a.jobs[0] = jobs_s;
+  if (!kCompact) {                                                           // shared pages are given up when all sequences have been planned
+    for (int j = tid; j < jobs_s; j += kPlanThreads) {
+      const int old = a.jobs[1 + 2 * j];
+      if (atomicSub(&c.refs[old], 1) == 1) { atomicOr(&c.free[old >> 5], 1u << (old & 31)); atomicMin(c.hint, old >> 5); }
+    }
+    if (tid == 0) a.jobs[0] = jobs_s;
+  }
 }
 
 // A cluster of kPlanBlocks: its first block plans, then all of them copy the pages that sequences shared and are to write to

@@ -118,3 +118,22 @@ def test_a_negative_amplitude_turns_keys_into_the_negatives_of_a_positive_one_s(
         q, out = torch.randn(2, 4, 1, 64, device="cuda").to(torch.bfloat16) * 0, torch.zeros(2, 4, 1, 64, device="cuda")
         B.dkv_cache8_attend(c.h, 0, 2, 1, q, out)
         assert (out == 0).all()                                              # logits of 0 * key: NaN were a key NaN or infinite
+
+
+@pytest.mark.parametrize("n_pages", [3150, 2200])                            # pages for everybody; too few
+def test_forks_among_more_sequences_than_the_planner_takes_at_a_time(n_pages):
+    """Who copies a shared page, and which pages are free, goes by what the call finds, for all its sequences."""
+    n = 2100
+    with Both(n_pages=n_pages, n_seqs=n, max_pages=2, Hkv=1, G=1) as c:
+        c.add(0, n // 2, 1, [i % 3 + 30 for i in range(n // 2)], 3, cap=32)  # 32: full pages, which are not copied
+        B.dkv_cache8_fork(c.h, 0, n // 2, n // 2, 1)
+        c.o.fork([(i, i + n // 2) for i in range(n // 2)])
+        none, full = c.o.reserve(range(n), [1] * n)
+        B.dkv_cache8_reserve(c.h, 0, n, 1, None, 1)
+        c.check()
+        words = B.dkv_cache8_status(c.h)[1]
+        assert bool(words[0] & B.DKV_C8_NO_PAGES) == bool(none) and not full and words[2] == sum(r == 0 for r in c.o.refs())
+        assert bool(none) == (n_pages < 3150)
+        B.dkv_cache8_reserve(c.h, 0, n, 1, None, 1)                          # what was given back is found again
+        c.o.reserve(range(n), [1] * n)
+        c.check()
