@@ -143,8 +143,8 @@ struct AttendWarp {
           q[i][p * 4 + k][1] = pack_half(y[2] * up, y[3] * up);
         }
       limit[i] = row < a.rows ? len - (a.causal ? a.nq - 1 - row % a.nq : 0) : len;
-      ref[i] = none == 0.f ? -INFINITY : 0.f;        // logits of such a row give no reference; its result shall be NaN
-      sum[i] = 0.f;
+      ref[i] = none == 0.f ? -INFINITY : 0.f;        // logits of such a row give no reference; its result is NaN, also where all are -infinity
+      sum[i] = limit[i] > 0 ? none : 0.f;
     }
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;

@@ -137,3 +137,19 @@ def test_forks_among_more_sequences_than_the_planner_takes_at_a_time(n_pages):
         B.dkv_cache8_reserve(c.h, 0, n, 1, None, 1)                          # what was given back is found again
         c.o.reserve(range(n), [1] * n)
         c.check()
+
+
+@pytest.mark.parametrize("n", [1, 80])                                       # slices of blocks, of warps
+@pytest.mark.parametrize("rows", [20, 700])
+def test_an_infinite_query_whose_logits_are_all_minus_infinity_gives_nan(n, rows):
+    with Both(n_pages=n * 24, n_seqs=n, max_pages=24) as c:
+        k = torch.randn(n, 2, rows, 64, device="cuda").abs().to(torch.bfloat16) + 0.5
+        put(c, 0, n, k, k)
+        q = torch.randn(n, 4, 2, 64, device="cuda").to(torch.bfloat16)
+        q[0, 1, 1, 5] = float("-inf")
+        out, lse = torch.zeros(q.shape, device="cuda"), torch.zeros(q.shape[:3], device="cuda")
+        B.dkv_cache8_attend(c.h, 0, n, 1, q, out, lse)
+        odd = torch.zeros(n, 4, 2, dtype=torch.bool, device="cuda")
+        odd[0, 1, 1] = True
+        assert torch.isnan(out[odd]).all() and torch.isnan(lse[odd]).all()
+        assert torch.isfinite(out[~odd]).all() and torch.isfinite(lse[~odd]).all()
