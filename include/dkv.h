@@ -393,7 +393,7 @@ typedef struct {
 typedef struct dkv_cache8 dkv_cache8;
 
 /* Create a cache without rows on the current device (host call; one allocation of n_pages * 2 * n_kv_heads * (R * head_dim + 4)
- * bytes of pages, 8 * n_seqs * max_pages of tables, 1536 * (head_dim + 2) an SM for dkv_cache8_attend, and some per page and sequence).  It belongs to that device and to one stream at
+ * bytes of pages, 8 * n_seqs * max_pages of tables, 1536 * (head_dim + 4) an SM for dkv_cache8_attend, and some per page and sequence).  It belongs to that device and to one stream at
  * a time: calls on it, replays of graphs that hold such calls included, follow one another.
  * Errors: INVALID_ARG, UNSUPPORTED, NOMEM, CUDA.  On error *out is NULL. */
 int dkv_cache8_create(const dkv_cache8_config* cfg, dkv_cache8** out);
@@ -423,7 +423,8 @@ int dkv_cache8_read(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const
  *   out = softmax(q . K^T / sqrt(head_dim)) V,  fp32 [n, n_q_heads, nq, head_dim];
  *   lse : fp32 [n, n_q_heads, nq], the natural logarithm of the denominators (NULL: not wanted).
  * causal != 0: the queries are those of the last nq rows, query j sees all rows but the last nq-1-j.  A query that sees no row
- * gets 0 and -infinity.  n_q_heads / n_kv_heads * nq <= 64.  Deterministic. */
+ * gets 0 and -infinity, one with an infinity or NaN that sees some NaN.  Values of every size are summed without overflow, whatever the
+ * length; what pages with a value scale below 2^-126 of the sequence's largest add loses bits.  n_q_heads / n_kv_heads * nq <= 64.  Deterministic. */
 int dkv_cache8_attend(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const dkv_rows* q, const dkv_rows* out, float* lse,
                       int32_t causal, void* stream);
 /* Sequences to, to + step, .. become forks of from, from + step, ..: what they held is given back, and they share the source's

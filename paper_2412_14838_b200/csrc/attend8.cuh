@@ -7,7 +7,7 @@
 // above: what is 2^-17 of it and more keeps its 8 or 11 bits, what is smaller is off by 2^-38 of it.  Weights are split into two
 // fp16 parts, 22 bits, which lie in the two halves of the 16-row operand where there are at most 8 query rows a head.
 //   S = Q K^T   scaled by the page's key scale when it leaves the accumulators;
-//   O = P V     a page's product is added to the result times its value scale.
+//   O = P V     a page's product is added to the result times its value scale, in units of the largest value scale met so far.
 // Weights are relative to a reference that a row's largest logit may pass by a factor of 2^7 before it is moved, so that in most steps
 // nothing is exchanged between lanes and the result is not rescaled.
 //
@@ -21,14 +21,13 @@
 // works on a chunk while the next kAttendStages - 1 are on their way.
 #pragma once
 #include "cache8.cuh"
-#include "merge.cuh"
 #include "ring.cuh"
 
 namespace dkv {
 
 constexpr int kAttendWarps = 12, kAttendStages = 2, kAttendRows = 32;
 constexpr int kAttendMaxSeqs = 1024;        // sequences a launch (their lengths and groups' prefix sums are in shared memory)
-constexpr float kDown = 5.9604644775390625e-8f;  // 2^-24: results are summed that much smaller, so that values up to the largest bf16 numbers sum without overflow
+constexpr float kSixteenth = 0.0625f;       // blocks leave averages that much smaller: the largest value, 448 * 2^120, passes fp32 (of results below 2^-122 bits are lost)
 constexpr float kLift = 8.f, kSlack = 7.f;  // weights are 2^(logit - reference + kLift); logits may pass the reference by kSlack: 2^15 fits fp16
 
 struct AttendArgs {
@@ -37,7 +36,7 @@ struct AttendArgs {
   float* out;                // [n][Hq][nq][D], strides below
   long long out_batch, out_head, out_token;
   float* lse;                // [n][Hq][nq] or null
-  float* scratch;            // [2 slices][rows of a head, in whole QB] partial results, (reference, sum) behind them
+  float* scratch;            // [2 slices][rows of a head, in whole QB] partial results, what belongs to each row behind them
   unsigned int* tickets;     // [n * Hkv], zero between launches
   long long wait;            // clock ticks after which a wait for a copy gives up
   int withhold;              // test hook: the chunk that warp 0 of block 0 never asks for, -1: none
@@ -82,8 +81,21 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
   return sum == 0.f ? -INFINITY : (ref - kLift + log2f(sum)) * 0.6931471805599453f;
 }
 
-// What takes a sum of weighted values to the result; a query that sees no row has sums of 0.
-__device__ __forceinline__ float up(float sum) { return sum == 0.f ? 0.f : 1.f / (kDown * sum); }
+// What belongs to a partial result, a sum of weighted values in units of `up`: the reference and the sum of the weights; the unit, a
+// power of two, 2^-126 or more, the largest value scale met.  In such units a sum stays below 2^48 over 2^24 rows, whatever the values; pages
+// whose scale is below 2^-126 of the largest in the sequence lose bits of what they add, below 2^-149 all of it.
+struct Part { float ref, sum, up; };
+__device__ __forceinline__ float over(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }      // 1 / x, a power of two from 2^-126 to 2^126
+// The factor of a part's sums relative to m.  A part may have no row that this query sees.
+__device__ __forceinline__ float weight_of(float ref, float sum, float m) { return sum == 0.f ? 0.f : fast_exp2(ref - m); }
+// A result from its sums; a query that sees no row has sums of 0.
+struct Whole {
+  float inv, up;
+  __device__ __forceinline__ Whole(float sum, float up) : inv(sum == 0.f ? 0.f : 1.f / sum), up(up) {}
+  __device__ __forceinline__ float4 of(float4 v) const { return make_float4(v.x * inv * up, v.y * inv * up, v.z * inv * up, v.w * inv * up); }
+};
+__device__ __forceinline__ void put_part(float* at, int row, const Part& p) { __stcg(reinterpret_cast<float4*>(at) + row, make_float4(p.ref, p.sum, p.up, 0.f)); }
+__device__ __forceinline__ Part get_part(const float* at, int row) { const float4 v = __ldcg(reinterpret_cast<const float4*>(at) + row); return {v.x, v.y, v.z}; }
 __device__ __forceinline__ float* out_row(const AttendArgs& a, int i, int h, int row) { return a.out + i * a.out_batch + (h * a.G + row / a.nq) * a.out_head + row % a.nq * a.out_token; }
 __device__ __forceinline__ void store_lse(const AttendArgs& a, int Hkv, int i, int h, int row, float ref, float sum) {
   if (a.lse) a.lse[((size_t)(i * Hkv + h) * a.G + row / a.nq) * a.nq + row % a.nq] = log_sum(ref, sum);
@@ -98,6 +110,7 @@ struct AttendWarp {
   float acc[kTiles][4];
   float ref[kHalves], sum[kHalves], qs[kHalves];     // reference (log2), sum of this lane's weights, scale2 / the query's scale
   int limit[kHalves];                                // rows the query sees
+  float up;                                          // the unit of `acc`, the largest value scale so far
 
   // The queries' raw numbers, asked for ahead of what their rows need.
   struct Raw { uint4 v[kHalves][kPanels][2]; };
@@ -148,10 +161,12 @@ struct AttendWarp {
     }
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+    up = 0x1p-126f;
   }
 
-  // 32 rows from `row` on; k: in shared memory, v: this lane's first piece there; ks, vs: the page's scales.
-  __device__ __forceinline__ void add(const uint4* k, const uint4* v, float ks, float vs, int row, int lane, int t) {
+  // 32 rows from `row` on; k: in shared memory, v: this lane's first piece there; ks, vs: the page's scales, vs in units of `up`, which has
+  // grown by 1 / shrink.
+  __device__ __forceinline__ void add(const uint4* k, const uint4* v, float ks, float vs, float shrink, int row, int lane, int t) {
     float s[4][4];                                   // 8 rows each: four sums that do not wait for one another
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
@@ -172,7 +187,7 @@ struct AttendWarp {
         }
       }
     }
-    bool past = false;
+    bool past = shrink != 1.f;
     float most[kHalves];
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
@@ -197,8 +212,9 @@ struct AttendWarp {
         m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
         m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
         m = fmaxf(m, ref[h]);
-        const float c = m == -INFINITY ? 1.f : fast_exp2(ref[h] - m);       // (the other query rows' references may still be -inf)
+        float c = m == -INFINITY ? 1.f : fast_exp2(ref[h] - m);             // (the other query rows' references may still be -inf)
         ref[h] = m; sum[h] *= c;
+        c *= shrink;
 #pragma unroll
         for (int j = 0; j < kTiles; ++j) {
           if (QB == 8) { acc[j][0] *= c; acc[j][1] *= c; acc[j][2] *= c; acc[j][3] *= c; }
@@ -257,20 +273,21 @@ struct AttendWarp {
   }
   // Dims 16 m + 4 t .. + 3 of query row g + 8 h.
   __device__ __forceinline__ float4 piece(int h, int m) const { return make_float4(acc[2 * m][2 * h], acc[2 * m][2 * h + 1], acc[2 * m + 1][2 * h], acc[2 * m + 1][2 * h + 1]); }
-  // Results as rows in part[QB][D + 4], (reference, sum) in ml[QB].
-  __device__ __forceinline__ void park(float* part, float2* ml, int g, int t) const {
+  __device__ __forceinline__ Part sums(int h) const { return {ref[h], sum[h], up}; }
+  // Results as rows in part[QB][D + 4], their sums in of[QB].
+  __device__ __forceinline__ void park(float* part, Part* of, int g, int t) const {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      if (t == 0) ml[g + 8 * h] = make_float2(ref[h], sum[h]);
+      if (t == 0) of[g + 8 * h] = sums(h);
 #pragma unroll
       for (int m = 0; m < D / 16; ++m) *reinterpret_cast<float4*>(part + (g + 8 * h) * (D + 4) + 16 * m + 4 * t) = piece(h, m);
     }
   }
-  // A result as it lies in the registers: [kHalves][D/16][32] pieces, then (reference, sum) of every row.
+  // A result as it lies in the registers: [kHalves][D/16][32] pieces, then the sums of every row.
   __device__ __forceinline__ void save(float* part, int lane, int g, int t) const {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      if (t == 0) __stcg(reinterpret_cast<float2*>(part + QB * D) + g + 8 * h, make_float2(ref[h], sum[h]));
+      if (t == 0) put_part(part + QB * D, g + 8 * h, sums(h));
 #pragma unroll
       for (int m = 0; m < D / 16; ++m) __stcg(reinterpret_cast<float4*>(part) + (h * (D / 16) + m) * 32 + lane, piece(h, m));
     }
@@ -279,6 +296,7 @@ struct AttendWarp {
   template <typename F>
   __device__ __forceinline__ void merge(F part, int parts, int lane, int g) {
     constexpr int kFlight = D == 64 ? 6 : 2;         // parts whose loads are in flight together, as many as the registers take
+    float unit = 0.f;                                // the same for all of a part's rows
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       float m = -INFINITY, l = 0.f;
@@ -286,26 +304,28 @@ struct AttendWarp {
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) r[x] = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int p0 = 0; p0 < parts; p0 += 8) {
-        float2 ml[8];
+        Part of[8];
 #pragma unroll
-        for (int f = 0; f < 8; ++f) ml[f] = __ldcg(reinterpret_cast<const float2*>(part(min(p0 + f, parts - 1)) + QB * D) + g + 8 * h);
+        for (int f = 0; f < 8; ++f) of[f] = get_part(part(min(p0 + f, parts - 1)) + QB * D, g + 8 * h);
 #pragma unroll
-        for (int f = 0; f < 8; ++f) m = fmaxf(m, ml[f].x);
+        for (int f = 0; f < 8; ++f) { m = fmaxf(m, of[f].ref); unit = fmaxf(unit, of[f].up); }
       }
+      const float down = over(unit);
       for (int p0 = 0; p0 < parts; p0 += kFlight) {
-        float2 ml[kFlight];
+        Part of[kFlight];
         float4 y[kFlight][D / 16];
 #pragma unroll
         for (int f = 0; f < kFlight; ++f) {
           const float* from = part(min(p0 + f, parts - 1));
-          ml[f] = __ldcg(reinterpret_cast<const float2*>(from + QB * D) + g + 8 * h);
+          of[f] = get_part(from + QB * D, g + 8 * h);
 #pragma unroll
           for (int x = 0; x < D / 16; ++x) y[f][x] = __ldcg(reinterpret_cast<const float4*>(from) + (h * (D / 16) + x) * 32 + lane);
         }
 #pragma unroll
         for (int f = 0; f < kFlight; ++f) {
-          const float k = p0 + f < parts && ml[f].y != 0.f ? fast_exp2(ml[f].x - m) : 0.f;      // (a part may have no row that this query sees)
-          l = p0 + f < parts ? fmaf(ml[f].y, k, l) : l;
+          float k = weight_of(of[f].ref, of[f].sum, m);
+          l = p0 + f < parts ? fmaf(of[f].sum, k, l) : l;
+          k *= of[f].up * down;
           if (p0 + f < parts) {
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) { r[x].x = fmaf(y[f][x].x, k, r[x].x); r[x].y = fmaf(y[f][x].y, k, r[x].y); r[x].z = fmaf(y[f][x].z, k, r[x].z); r[x].w = fmaf(y[f][x].w, k, r[x].w); }
@@ -316,20 +336,18 @@ struct AttendWarp {
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) { acc[2 * x][2 * h] = r[x].x; acc[2 * x][2 * h + 1] = r[x].y; acc[2 * x + 1][2 * h] = r[x].z; acc[2 * x + 1][2 * h + 1] = r[x].w; }
     }
+    up = unit;
   }
   __device__ __forceinline__ void store(const AttendArgs& a, int Hkv, int i, int h, int g, int t) const {
 #pragma unroll
     for (int k = 0; k < kHalves; ++k) {
       const int row = g + 8 * k;
       if (row >= a.rows) continue;
-      const float inv = up(sum[k]);
+      const Whole whole(sum[k], up);
       float* to = out_row(a, i, h, row);
       if (t == 0) store_lse(a, Hkv, i, h, row, ref[k], sum[k]);
 #pragma unroll
-      for (int m = 0; m < D / 16; ++m) {
-        const float4 v = piece(k, m);
-        *reinterpret_cast<float4*>(to + 16 * m + 4 * t) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-      }
+      for (int m = 0; m < D / 16; ++m) *reinterpret_cast<float4*>(to + 16 * m + 4 * t) = whole.of(piece(k, m));
     }
   }
 };
@@ -411,10 +429,18 @@ struct Ring {
     };
     auto wait = [&](int place, int parity) { return __all_sync(0xFFFFFFFFu, ring_wait(bar_s + place * 8, parity, limit)) != 0; };
     auto use = [&](int x, int place) {
-      if ((x & 31) == 0) now = sc;
-      const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = kDown * __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
+      float shrink = 1.f;
+      if ((x & 31) == 0) {                             // the unit is the largest value scale of all chunks looked up
+        now = sc;
+        const float top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, x + lane < count ? __float_as_uint(sc.y) : 0u));
+        if (top > w.up) {
+          if (x) shrink = w.up * over(top);
+          w.up = top;
+        }
+      }
+      const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = over(w.up) * __shfl_sync(0xFFFFFFFFu, now.y, x & 31);
       const unsigned char* k = at + place * kChunkBytes;
-      w.add(reinterpret_cast<const uint4*>(k), reinterpret_cast<const uint4*>(k + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, first + x * step * kAttendRows, lane, t);
+      w.add(reinterpret_cast<const uint4*>(k), reinterpret_cast<const uint4*>(k + kHalfBytes) + t * 8 + ((g + 2 * t) & 7), ks, vs, shrink, first + x * step * kAttendRows, lane, t);
     };
     static_assert(kAttendStages <= 32);                // chunk 32 i is used before the scales of chunk 32 (i + 1) are looked up
     look(0);
@@ -463,20 +489,25 @@ __device__ __forceinline__ HeadAt head_at(int u, const int* prefix_s, int n, int
   const int units = (prefix_s[lo + 1] - prefix_s[lo]) / Hkv, h = (u - prefix_s[lo]) / units;
   return {lo, h, prefix_s[lo] + h * units, units};
 }
-// As merge_warps, for `count` results: dims d .. d + 3 of query row qi.
-template <int D, int QB>
-__device__ __forceinline__ float2 merge_team(const float* part, const float2* ml, int count, int qi, int d, float4& v) {
-  float m = -INFINITY, l = 0.f;
-  for (int w = 0; w < count; ++w) m = fmaxf(m, ml[w * QB + qi].x);
+// The parked results of `count` warps (kCount where that is not 0) added up: dims d .. d + 3 of query row qi, and the row's sums.
+template <int D, int QB, int kCount>
+__device__ __forceinline__ Part merge_team(const float* part, const Part* of, int count, int qi, int d, float4& v) {
+  const int n = kCount ? kCount : count;
+  Part all = {-INFINITY, 0.f, 0.f};
   v = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int w = 0; w < count; ++w) {
-    const float2 p = ml[w * QB + qi];
-    const float k = p.y == 0.f ? 0.f : fast_exp2(p.x - m);                    // (a warp may have no row that this query sees)
+#pragma unroll (kCount ? kCount : 1)
+  for (int w = 0; w < n; ++w) { all.ref = fmaxf(all.ref, of[w * QB + qi].ref); all.up = fmaxf(all.up, of[w * QB + qi].up); }
+  const float down = over(all.up);
+#pragma unroll (kCount ? kCount : 1)
+  for (int w = 0; w < n; ++w) {
+    const Part p = of[w * QB + qi];
+    float k = weight_of(p.ref, p.sum, all.ref);
+    all.sum = fmaf(p.sum, k, all.sum);
+    k *= p.up * down;
     const float4 y = *reinterpret_cast<const float4*>(part + (w * QB + qi) * (D + 4) + d);
     v.x = fmaf(y.x, k, v.x); v.y = fmaf(y.y, k, v.y); v.z = fmaf(y.z, k, v.z); v.w = fmaf(y.w, k, v.w);
-    l = fmaf(p.y, k, l);
   }
-  return make_float2(m, l);
+  return all;
 }
 
 // Few heads.  The warps of a block form a team for every QB query rows (one team of twelve for up to 16 rows, four of three for 64):
@@ -490,7 +521,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, 1)
 attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendArgs a) {
   using Warp = AttendWarp<D, QB, kKind>;
   constexpr int NW = kAttendWarps;
-  static_assert(NW * QB * (D + 4) * 4 + NW * QB * 8 <= attend_smem<D>() && 256 * QB * 12 <= attend_smem<D>());   // merges, of at most 256 parts
+  static_assert(NW * QB * ((D + 4) * 4 + (int)sizeof(Part)) <= attend_smem<D>() && 256 * QB * 12 <= attend_smem<D>());   // merges, of at most 256 parts
   static_assert(NW % 2 == 0 && NW % 3 == 0 && NW % 4 == 0);                                                      // teams of equal size
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ int prefix_s[kAttendMaxSeqs + 1], len_s[kAttendMaxSeqs];
@@ -502,7 +533,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
   const int c0 = kTeams ? warp / size * QB : 0, member = kTeams ? warp % size : warp;             // this warp's first query row, and place in its team
   Ring<D> ring;
   float* part_s = reinterpret_cast<float*>(smem);
-  float2* ml_s = reinterpret_cast<float2*>(part_s + NW * QB * (D + 4));
+  Part* of_s = reinterpret_cast<Part*>(part_s + NW * QB * (D + 4));
   pdl_launch();
   ring.start(smem + (size_t)warp * Ring<D>::kBytes, bar_s + warp * kAttendStages, lane, a);
   look_ahead(c, a);
@@ -522,7 +553,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
     u = end;
     const int c_lo = slices.owner(at.u0), c_hi = slices.owner(at.u0 + at.units - 1);
     // parts: slot 0 of a slice continues a head, slot 1 begins one that others continue
-    auto part = [&](int sl, bool first, int team) { return a.scratch + ((size_t)(2 * sl + first) * teams + team) * (QB * (D + 2)); };
+    auto part = [&](int sl, bool first, int team) { return a.scratch + ((size_t)(2 * sl + first) * teams + team) * (QB * (D + 4)); };
     {
       Warp w;
       typename Warp::Raw raw;
@@ -532,21 +563,20 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
       if (ring.broken() && lane == 0) report(c, kTimeout, seq);
       __syncthreads();
       w.add_up();
-      w.park(part_s + warp * QB * (D + 4), ml_s + warp * QB, g, t);
+      w.park(part_s + warp * QB * (D + 4), of_s + warp * QB, g, t);
     }
     __syncthreads();
     for (int x = tid; x < a.rows * (D / 4); x += NW * 32) {
       const int row = x / (D / 4), d = x % (D / 4) * 4, team = row / QB, qi = row % QB;
       float4 v;
-      const float2 ml = kTeams ? merge_team<D, QB>(part_s + team * size * QB * (D + 4), ml_s + team * size * QB, size, qi, d, v) : merge_warps<D, QB, NW>(part_s, ml_s, x, v);
+      const Part of = merge_team<D, QB, kTeams ? 0 : NW>(part_s + team * size * QB * (D + 4), of_s + team * size * QB, size, qi, d, v);
       if (whole) {
-        const float inv = up(ml.y);
-        *reinterpret_cast<float4*>(out_row(a, lo, h, row) + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-        if (d == 0) store_lse(a, c.Hkv, lo, h, row, ml.x, ml.y);
+        *reinterpret_cast<float4*>(out_row(a, lo, h, row) + d) = Whole(of.sum, of.up).of(v);
+        if (d == 0) store_lse(a, c.Hkv, lo, h, row, of.ref, of.sum);
       } else {
         float* to = part(own, begins, team);
-        __stcg(reinterpret_cast<float4*>(to) + qi * (D / 4) + d / 4, v);
-        if (d == 0) __stcg(reinterpret_cast<float2*>(to + QB * D) + qi, ml);
+        __stcg(reinterpret_cast<float4*>(to) + qi * (D / 4) + d / 4, Whole(of.sum, of.up * kSixteenth).of(v));
+        if (d == 0) __stcg(reinterpret_cast<float2*>(to + QB * D) + qi, make_float2(of.ref, of.sum));
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the ring's copies come after what was written here
@@ -560,7 +590,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
     }
     __syncthreads();
     if (ticket_s != (unsigned int)(c_hi - c_lo)) continue;
-    // all parts of the head are there: their weights, by (part, query row), then every result as one weighted sum
+    // all parts of the head are there, averages of their values: their weights, by (part, query row), then every result as one weighted sum
     const int parts = c_hi - c_lo + 1;
     float* weight_s = reinterpret_cast<float*>(smem);
     float2* all_s = reinterpret_cast<float2*>(weight_s + parts * QB);
@@ -574,11 +604,11 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
         for (int p = lane; p < parts; p += 32) m = fmaxf(m, all_s[p * QB + qi].x);
 #pragma unroll
         for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        auto weight = [&](float2 ml) { return ml.y == 0.f ? 0.f : fast_exp2(ml.x - m); };      // (a part may have no row that this query sees)
-        for (int p = lane; p < parts; p += 32) l += weight(all_s[p * QB + qi]) * all_s[p * QB + qi].y;
+        auto weight = [&](float2 ml) { return weight_of(ml.x, ml.y, m) * ml.y; };
+        for (int p = lane; p < parts; p += 32) l += weight(all_s[p * QB + qi]);
 #pragma unroll
         for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-        const float inv = up(l);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         for (int p = lane; p < parts; p += 32) weight_s[p * QB + qi] = weight(all_s[p * QB + qi]) * inv;
         if (lane == 0) store_lse(a, c.Hkv, lo, h, r0 + qi, m, l);
       }
@@ -601,7 +631,7 @@ attend8_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ AttendA
               r.x = fmaf(y[f].x, k, r.x); r.y = fmaf(y[f].y, k, r.y); r.z = fmaf(y[f].z, k, r.z); r.w = fmaf(y[f].w, k, r.w);
             }
         }
-        *reinterpret_cast<float4*>(out_row(a, lo, h, r0 + qi) + x % (D / 4) * 4) = r;
+        *reinterpret_cast<float4*>(out_row(a, lo, h, r0 + qi) + x % (D / 4) * 4) = make_float4(r.x / kSixteenth, r.y / kSixteenth, r.z / kSixteenth, r.w / kSixteenth);
       }
       __syncthreads();
     }
@@ -655,7 +685,7 @@ attend8_warps_kernel(const __grid_constant__ Cache8 c, const __grid_constant__ A
     w.add_up();
     if (whole) { w.store(a, c.Hkv, at.i, at.h, g, t); continue; }
     const int c_lo = slices.owner(row0), c_hi = slices.owner(at.u0 + at.units - 1);
-    auto part = [&](int sl, bool first) { return a.scratch + (size_t)(2 * sl + first) * (QB * (D + 2)); };
+    auto part = [&](int sl, bool first) { return a.scratch + (size_t)(2 * sl + first) * (QB * (D + 4)); };
     w.save(part(own, first == 0), lane, g, t);
     unsigned int* ticket = a.tickets + (size_t)at.i * c.Hkv + at.h;
     __threadfence();

@@ -128,7 +128,7 @@ int attend_blocks(const dkv_cache8* c) { return std::min(c->n_sms, 256); }
 bool attend_by_warps(const dkv_cache8* c, int n, int rows) { return rows <= 16 && (long long)n * c->cfg.n_kv_heads > attend_blocks(c); }
 // Floats of scratch: two parts a slice, of 16 rows a warp or of all a block.
 size_t attend_scratch(const dkv_cache8* c) {
-  return (size_t)attend_blocks(c) * 2 * std::max(kAttendWarps * 16, kMostQueries) * (c->cfg.head_dim + 2);
+  return (size_t)attend_blocks(c) * 2 * std::max(kAttendWarps * 16, kMostQueries) * (c->cfg.head_dim + 4);
 }
 
 template <int D, int QB, int kKind>

@@ -153,3 +153,58 @@ def test_an_infinite_query_whose_logits_are_all_minus_infinity_gives_nan(n, rows
         odd[0, 1, 1] = True
         assert torch.isnan(out[odd]).all() and torch.isnan(lse[odd]).all()
         assert torch.isfinite(out[~odd]).all() and torch.isfinite(lse[~odd]).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -120, 1e-35, 1e-33, 1e-30])
+@pytest.mark.parametrize("n,Hkv,rows", [(1, 2, 3000), (1, 1, 40), (60, 3, 100)])      # slices of blocks, one slice, slices of warps
+def test_attention_over_values_near_the_smallest(size, n, Hkv, rows):
+    with Both(n_pages=n * (rows // 32 + 1) + 4, n_seqs=n, max_pages=rows // 32 + 1, Hkv=Hkv) as c:
+        k = torch.randn(n, Hkv, rows, 64, device="cuda").to(torch.bfloat16)
+        v = (torch.randn(n, Hkv, rows, 64, device="cuda") * size).to(torch.bfloat16)
+        put(c, 0, n, k, v)
+        c.attend(0, n, 1, 2, False)
+
+
+@pytest.mark.parametrize("G,nq", [(2, 1), (5, 3), (8, 4)])                   # 8 query rows a pass, 16, two teams
+def test_attention_over_pages_whose_values_are_far_apart(G, nq):
+    """Small values first and large ones behind them, and the other way round, in one warp's rows and in several blocks'."""
+    with Both(n_pages=300, n_seqs=2, max_pages=150, G=G) as c:
+        k = torch.randn(2, 2, 4000, 64, device="cuda").to(torch.bfloat16)
+        size = 2.0 ** torch.linspace(-110, 100, 4000, device="cuda")
+        v = torch.randn(2, 2, 4000, 64, device="cuda") * torch.stack([size, size.flip(0)])[:, None, :, None]
+        put(c, 0, 2, k, v.to(torch.bfloat16))
+        c.attend(0, 2, 1, nq, True)
+
+
+def test_many_large_values_whose_logits_pass_the_reference():
+    """The first rows of every warp have logits of 0, the others of 6.5 (log2): weights of 2^14.5, of which each warp adds up 960 times
+    values near the largest."""
+    blocks = torch.cuda.get_device_properties(0).multi_processor_count
+    with Both(n_pages=200, R=64, n_seqs=blocks, max_pages=200, Hkv=1, G=1) as c:
+        rows = 12000
+        k = torch.zeros(1, 1, rows, 64, device="cuda")
+        k[:, :, 12 * 32:, 0] = 36.0
+        v = torch.full((1, 1, rows, 64), 3e38, device="cuda")
+        put(c, 0, 1, k.to(torch.bfloat16), v.to(torch.bfloat16))
+        for s in range(1, blocks):                                           # a head a block: no slice shares one
+            B.dkv_cache8_fork(c.h, 0, s, 1, 1)
+        q = torch.zeros(blocks, 1, 1, 64, device="cuda")
+        q[..., 0] = 1.0
+        out, lse = torch.zeros(blocks, 1, 1, 64, device="cuda"), torch.zeros(blocks, 1, 1, device="cuda")
+        B.dkv_cache8_attend(c.h, 0, blocks, 1, q.to(torch.bfloat16), out, lse)
+        want, want_lse = c.o.attend(0, q[0].double().cpu().numpy(), False)
+        assert np.abs(out.double().cpu().numpy() / want[None] - 1).max() < 2.0 ** -19
+        assert np.abs(lse.double().cpu().numpy() - want_lse).max() < 1e-5
+
+
+def test_many_large_values_with_equal_logits():
+    """Weights of 2^8 each: a block adds up 90000 times 2^8 times values near the largest."""
+    blocks = torch.cuda.get_device_properties(0).multi_processor_count
+    with Both(n_pages=720, R=128, n_seqs=blocks, max_pages=720, Hkv=1, G=1) as c:
+        k = torch.zeros(1, 1, 90000, 64, device="cuda").to(torch.bfloat16)
+        put(c, 0, 1, k, torch.full_like(k, 3.2e38))
+        for s in range(1, blocks):                                           # a head a block: no slice shares one
+            B.dkv_cache8_fork(c.h, 0, s, 1, 1)
+        out = torch.zeros(blocks, 1, 1, 64, device="cuda")
+        B.dkv_cache8_attend(c.h, 0, blocks, 1, torch.zeros(blocks, 1, 1, 64, dtype=torch.bfloat16, device="cuda"), out)
+        assert np.abs(out.double().cpu().numpy() / c.o.rows(0, 1).max() - 1).max() < 2.0 ** -19
