@@ -464,7 +464,8 @@ int dkv_cache8_views(dkv_cache8* c, const int32_t** len, const int32_t** held, c
 }
 
 int dkv_cache8_status(dkv_cache8* c, int32_t* host_status) {
-  if (!c || !host_status) return DKV_ERR_INVALID_ARG;
+  if (int rc = check(c, 0, 0, 1)) return rc;                                 // another device's kernels would be waited for, not the cache's
+  if (!host_status) return DKV_ERR_INVALID_ARG;
   C8_CUDA(c, cudaDeviceSynchronize());
   int status[2];
   const int clear[2] = {0, INT_MAX}, words = (c->cfg.n_pages + 31) / 32;

@@ -1,5 +1,7 @@
 """The cache in 8 bits at the ends of its range, against the oracle: values near the largest and smallest numbers, long sums,
 more sequences than one pass of the planner takes, and calls that only documents allow."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -208,3 +210,29 @@ def test_many_large_values_with_equal_logits():
         out = torch.zeros(blocks, 1, 1, 64, device="cuda")
         B.dkv_cache8_attend(c.h, 0, blocks, 1, torch.zeros(blocks, 1, 1, 64, dtype=torch.bfloat16, device="cuda"), out)
         assert np.abs(out.double().cpu().numpy() / c.o.rows(0, 1).max() - 1).max() < 2.0 ** -19
+
+
+def test_every_call_wants_the_cache_s_own_device():
+    """The device that a cache remembers, behind its configuration, is put to another number than the current one's."""
+    with Both(n_seqs=2) as c:
+        c.add(0, 2, 1, [10, 20], 1)
+        k = torch.zeros(2, 2, 1, 64, dtype=torch.bfloat16, device="cuda")
+        q, out = torch.zeros(2, 4, 1, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 4, 1, 64, device="cuda")
+        device = ctypes.c_int32.from_address(c.h + ctypes.sizeof(B.DkvCache8Config))
+        assert device.value == torch.cuda.current_device()
+        calls = [lambda: B.dkv_cache8_reserve(c.h, 0, 2, 1, None, 1), lambda: B.dkv_cache8_append(c.h, 0, 2, 1, k, k),
+                 lambda: B.dkv_cache8_read(c.h, 0, 2, 1, k, k), lambda: B.dkv_cache8_attend(c.h, 0, 2, 1, q, out),
+                 lambda: B.dkv_cache8_fork(c.h, 0, 1, 1, 1), lambda: B.dkv_cache8_compact(c.h, 0, 2, 1, torch.zeros(2, 2, 0, dtype=torch.int32, device="cuda")),
+                 lambda: B.dkv_cache8_trim(c.h, 0, 2, 1, None, 1)]
+        torch.cuda.synchronize()
+        device.value += 1
+        try:
+            for call in calls:
+                with pytest.raises(B.DkvError) as e:
+                    call()
+                assert e.value.code == B.DKV_ERR_INVALID_ARG
+            assert B.dkv_cache8_status(c.h)[0] == B.DKV_ERR_INVALID_ARG
+        finally:
+            device.value -= 1
+        assert B.dkv_cache8_status(c.h)[0] == B.DKV_OK
+        c.check()
