@@ -406,8 +406,8 @@ int dkv_cache8_destroy(dkv_cache8* c);
 
 /* Room for rows[i] more rows of the i-th sequence (rows: int32 [n], device; NULL: `add` each).  The lowest free pages are given
  * out in the order of the sequences.  Where pages do not last, the first sequence that cannot be served and all after it in
- * this call get none.  A sequence whose last page is partly filled and shared with a fork gets its own copy of it.  Rows
- * reserved earlier and not yet added count. */
+ * this call get none.  A sequence whose last page is partly filled and shared with a fork gets its own copy of it (all of them, where
+ * all that share it ask in one call).  Rows reserved earlier and not yet added count. */
 int dkv_cache8_reserve(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* rows, int32_t add, void* stream);
 /* The first rows[i] of k[i], v[i] ([n, n_kv_heads, tokens, head_dim]) go behind the rows of the i-th sequence
  * (rows: int32 [n], device, at most `tokens`; NULL: all).  With `rotary` the keys are turned first, row j by position
@@ -437,7 +437,7 @@ int dkv_cache8_fork(dkv_cache8* c, int32_t from, int32_t to, int32_t n, int32_t 
  * stays as it is, and is reported).  A row number outside the sequence is reported and gives a row of zeros. */
 int dkv_cache8_compact(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* idx, int32_t heads, int32_t cols,
                        const int32_t* count, void* stream);
-/* Cut sequences to keep[i] rows (int32 [n], device; more than there are: no cut), or where keep is NULL by `drop` >= 0 rows
+/* Cut sequences to keep[i] rows (int32 [n], device; more than there are: no cut; fewer than 0: 0, and reported), or where keep is NULL by `drop` >= 0 rows
  * (as far as there are).  Pages behind the last row are given back, reserved ones too: drop = INT32_MAX frees a sequence. */
 int dkv_cache8_trim(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const int32_t* keep, int32_t drop, void* stream);
 /* Device-side views, owned by the cache (any may be NULL): len int32 [n_seqs] rows, held int32 [n_seqs] pages, table int32

@@ -11,11 +11,11 @@
 // Weights are relative to a reference that a row's largest logit may pass by a factor of 2^7 before it is moved, so that in most steps
 // nothing is exchanged between lanes and the result is not rescaled.
 //
-// Measured: 64 sequences of 8K rows, 8 KV heads of 128 dims, 4 query rows: 1.07 GB in 179 us, 6.0 TB/s, 0.92 of the measured copy rate.
+// Measured: 64 sequences of 8K rows, 8 KV heads of 128 dims, 4 query rows: 1.07 GB in 177 us, 6.1 TB/s, 0.92 of the measured copy rate.
 // Of what it took to get there: codes by 16-byte copies of every lane were 4.7 TB/s at best, whatever the number in flight; four
 // independent sums in the first product and twelve warps instead of eight, 278 -> 253 us; a reference that rarely moves.
 // Short ones are bound by latency: a sequence of 160 rows takes 6 us, of which 3 is the chain length, table, codes; one of 32K rows
-// with 16 query rows 28, 12 for its codes, 4.4 before them, 2.5 to merge a block's warps and 6 the blocks' parts.
+// with 16 query rows 28, with 64 75 (every team converts every code), 12 for its codes, 4.4 before them, 2.5 to merge a block's warps and 6 the blocks' parts.
 //
 // Every warp has a ring of its own in shared memory, filled by bulk copies (4 or 8 KB, one or two instructions a chunk of 32 rows): it
 // works on a chunk while the next kAttendStages - 1 are on their way.

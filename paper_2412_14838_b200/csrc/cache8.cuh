@@ -308,8 +308,10 @@ __device__ __forceinline__ int no_room(const Cache8& c, const AppendArgs& a, con
 // 16-bit numbers in registers straight to codes, and asks for the next one's rows before it works on this one's.  Bound by HBM (2
 // bytes in, 1 out), but for the chain of loads at a block's start and the ticket at its end, which is why a block has several heads
 // where there are blocks enough.  Angles are shared by all heads (shared memory, [R][rot/2]).  32 sequences of 544 rows, 8 heads of 128:
-// 23.5 us for 107 MB (4.5 TB/s); a block a head and tensor took 44, a warp each 40, rings of cp.async in place of the registers that
-// hold the next rows 31.  What bounds it is its instructions, some fourteen a number to begin with, half of that now.  grid (pages a sequence can touch,
+// 24 us for 107 MB (4.4 TB/s); a block a head and tensor took 44, a warp each 40, rings of cp.async in place of the registers that
+// hold the next rows 31.  What bounds it is its instructions, some fourteen a number to begin with, half of that now.
+// Keys turned in neighbouring pairs: 33 us for 100 MB (28 unturned); in halves 135 for 197 MB (43 unturned): the other half of a row
+// is loaded when it is needed, not ahead.  grid (pages a sequence can touch,
 // 2 Hkv / per, n); the last block of a sequence to arrive (a ticket) makes the rows part of it.
 constexpr int kQuadThreads = 512;                                            // R * D / 32 threads, at most
 template <int D, int kKind, int kIo, bool kTurn>
