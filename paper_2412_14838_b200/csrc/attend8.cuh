@@ -27,6 +27,7 @@ namespace dkv {
 
 constexpr int kAttendWarps = 12, kAttendStages = 2, kAttendRows = 32;
 constexpr int kAttendMaxSeqs = 1024;        // sequences a launch (their lengths and groups' prefix sums are in shared memory)
+constexpr long long kDrainTicks = 2000000;  // about a millisecond, for copies on their way when a wait runs out, however short its own limit
 constexpr float kSixteenth = 0.0625f;       // blocks leave averages that much smaller: the largest value, 448 * 2^120, passes fp32 (of results below 2^-122 bits are lost)
 constexpr float kLift = 8.f, kSlack = 7.f;  // weights are 2^(logit - reference + kLift); logits may pass the reference by kSlack: 2^15 fits fp16
 
@@ -428,6 +429,7 @@ struct Ring {
       return !withheld;
     };
     auto wait = [&](int place, int parity) { return __all_sync(0xFFFFFFFFu, ring_wait(bar_s + place * 8, parity, limit)) != 0; };
+    auto drain = [&](int place, int parity) { ring_wait(bar_s + place * 8, parity, limit > kDrainTicks ? limit : kDrainTicks); __syncwarp(); };
     auto use = [&](int x, int place) {
       float shrink = 1.f;
       if ((x & 31) == 0) {                             // the unit is the largest value scale of all chunks looked up
@@ -444,7 +446,7 @@ struct Ring {
     };
     static_assert(kAttendStages <= 32);                // chunk 32 i is used before the scales of chunk 32 (i + 1) are looked up
     look(0);
-    places.run(count, ask, [&] { w.start(raw, a, c0, len, g); }, wait, use);
+    places.run(count, ask, [&] { w.start(raw, a, c0, len, g); }, wait, use, drain);
   }
 };
 

@@ -26,10 +26,10 @@ struct RingPlaces {
 
   // Runs chunks 0 .. count - 1 through the ring, kStages - 1 of them ahead of the one that is worked on.  ask(x, place): asks for chunk x;
   // whether a copy was started.  wait(place, parity): false where the wait ran out.  use(x, place).  begin(): once the first chunks are asked
-  // for.  Where a wait runs out the copies that were started are waited for once more, with the same limit, right there: the memory is
-  // the caller's again.  The counters stay where they were then: what they say of the phases holds for what was on its way.
-  template <typename Ask, typename Begin, typename Wait, typename Use>
-  DKV_HOST_DEVICE void run(int count, Ask ask, Begin begin, Wait wait, Use use) {
+  // for.  Where a wait runs out the copies that were started are waited for right there, by drain(place, parity), which has a limit of its
+  // own: the memory is the caller's again.  The counters stay where they were then: what they say of the phases holds for what was on its way.
+  template <typename Ask, typename Begin, typename Wait, typename Use, typename Drain>
+  DKV_HOST_DEVICE void run(int count, Ask ask, Begin begin, Wait wait, Use use, Drain drain) {
     auto fetch = [&](int x, int at) { if (x < count && ask(x, at)) asked |= 1u << at; };
     if (!broken) {
 #ifdef __CUDACC__
@@ -44,7 +44,7 @@ struct RingPlaces {
       if (!wait(stage, phase)) {
         broken = true;
         for (int at = 0; at < kStages; ++at)
-          if (asked >> at & 1) wait(at, parity(at));
+          if (asked >> at & 1) drain(at, parity(at));
         asked = 0;
         return;
       }

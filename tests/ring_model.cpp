@@ -35,11 +35,10 @@ void heads(const std::vector<int>& counts, int late, bool withheld) {
         [&] { ++begun; },
         [&](int at, int parity) {
           Place& p = places[at];
-          CHECK(!was_broken && p.expects);
+          CHECK(!was_broken && !failed && p.expects);
           CHECK((p.phases & 1) == parity);                   // another parity: the test is true at once, whatever is on its way
-          if (!failed && used == late) { ++failed; return false; }
-          CHECK(p.copy);                                     // never waits for what was not asked for
-          drained += failed;
+          if (used == late) { ++failed; return false; }
+          CHECK(p.copy);
           p.copy = p.expects = false;
           ++p.phases;
           return true;
@@ -49,6 +48,14 @@ void heads(const std::vector<int>& counts, int late, bool withheld) {
           places[at].holds = -1;
           ++next;
           ++used;
+        },
+        [&](int at, int parity) {
+          Place& p = places[at];
+          CHECK(failed && (p.phases & 1) == parity);
+          CHECK(p.copy);                                     // never waits for what was not asked for
+          p.copy = p.expects = false;
+          ++p.phases;
+          ++drained;
         });
     CHECK(begun == 1);
     for (const Place& p : places) CHECK(!p.copy);            // whatever was started has ended when run() returns

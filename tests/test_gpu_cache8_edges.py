@@ -236,3 +236,26 @@ def test_every_call_wants_the_cache_s_own_device():
             device.value -= 1
         assert B.dkv_cache8_status(c.h)[0] == B.DKV_OK
         c.check()
+
+
+@pytest.mark.parametrize("n,Hkv", [(1, 2), (60, 3)])                        # a slice a block, a slice a warp
+def test_the_shortest_limit_of_waits_leaves_nothing_behind(n, Hkv):
+    """1000 clock ticks are fewer than a copy takes: warps stop at their first chunk, wait for the copies that they have started, and
+    the next call with a usual limit finds the cache, and its scratch, as ever."""
+    with Both(n_pages=4000, n_seqs=n, max_pages=4000 // n, Hkv=Hkv, D=128, oracle=False) as c:
+        rows = 60000 if n == 1 else 2000
+        k, v = (torch.randn(n, Hkv, rows, 128, device="cuda").to(torch.bfloat16) for _ in range(2))
+        B.dkv_cache8_reserve(c.h, 0, n, 1, None, rows)
+        B.dkv_cache8_append(c.h, 0, n, 1, k, v)
+        q = torch.randn(n, Hkv * 2, 4, 128, device="cuda").to(torch.bfloat16)
+        good, out = torch.zeros(q.shape, device="cuda"), torch.zeros(q.shape, device="cuda")
+        B.dkv_cache8_attend(c.h, 0, n, 1, q, good)
+        for _ in range(3):
+            B.dkv_cache8_set_wait_limit(c.h, 1000)
+            for _ in range(5):
+                B.dkv_cache8_attend(c.h, 0, n, 1, q, out)
+            code, words = B.dkv_cache8_status(c.h)
+            assert code == (B.DKV_ERR_TIMEOUT if words[0] else B.DKV_OK) and words[0] in (0, B.DKV_C8_TIMEOUT)
+            B.dkv_cache8_set_wait_limit(c.h, 4_000_000_000)
+            B.dkv_cache8_attend(c.h, 0, n, 1, q, out)
+            assert torch.equal(out, good) and B.dkv_cache8_status(c.h)[0] == B.DKV_OK
