@@ -424,7 +424,7 @@ int dkv_cache8_read(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const
  *   lse : fp32 [n, n_q_heads, nq], the natural logarithm of the denominators (NULL: not wanted).
  * causal != 0: the queries are those of the last nq rows, query j sees all rows but the last nq-1-j.  A query that sees no row
  * gets 0 and -infinity, one with an infinity or NaN that sees some NaN.  Values of every size are summed without overflow, whatever the
- * length; what pages with a value scale below 2^-126 of the sequence's largest add loses bits.  n_q_heads / n_kv_heads * nq <= 64.  Deterministic. */
+ * length; what pages with a value scale below 2^-204 of the sequence's largest add loses bits.  n_q_heads / n_kv_heads * nq <= 64.  Deterministic. */
 int dkv_cache8_attend(dkv_cache8* c, int32_t first, int32_t n, int32_t step, const dkv_rows* q, const dkv_rows* out, float* lse,
                       int32_t causal, void* stream);
 /* Sequences to, to + step, .. become forks of from, from + step, ..: what they held is given back, and they share the source's

@@ -7,7 +7,7 @@
 // above: what is 2^-17 of it and more keeps its 8 or 11 bits, what is smaller is off by 2^-38 of it.  Weights are split into two
 // fp16 parts, 22 bits, which lie in the two halves of the 16-row operand where there are at most 8 query rows a head.
 //   S = Q K^T   scaled by the page's key scale when it leaves the accumulators;
-//   O = P V     a page's product is added to the result times its value scale, in units of the largest value scale met so far.
+//   O = P V     a page's product is added to the result times its value scale, in units that follow the largest value scale met so far.
 // Weights are relative to a reference that a row's largest logit may pass by a factor of 2^7 before it is moved, so that in most steps
 // nothing is exchanged between lanes and the result is not rescaled.
 //
@@ -83,8 +83,9 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
 }
 
 // What belongs to a partial result, a sum of weighted values in units of `up`: the reference and the sum of the weights; the unit, a
-// power of two, 2^-126 or more, the largest value scale met.  In such units a sum stays below 2^48 over 2^24 rows, whatever the values; pages
-// whose scale is below 2^-126 of the largest in the sequence lose bits of what they add, below 2^-149 all of it.
+// power of two, 2^-78 of the largest value scale met, but 2^-36 at least: the ratio of any two times a weight down to 2^-46 is an fp32 number.
+// Over 2^24 rows, the most that there can be, a sum of codes times weights is below 2^48, and in such units below 2^126 whatever the scales;
+// pages whose scale is below 2^-204 of the largest lose bits of what they add.
 struct Part { float ref, sum, up; };
 __device__ __forceinline__ float over(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }      // 1 / x, a power of two from 2^-126 to 2^126
 // The factor of a part's sums relative to m.  A part may have no row that this query sees.
@@ -111,7 +112,7 @@ struct AttendWarp {
   float acc[kTiles][4];
   float ref[kHalves], sum[kHalves], qs[kHalves];     // reference (log2), sum of this lane's weights, scale2 / the query's scale
   int limit[kHalves];                                // rows the query sees
-  float up;                                          // the unit of `acc`, the largest value scale so far
+  float up;                                          // the unit of `acc`
 
   // The queries' raw numbers, asked for ahead of what their rows need.
   struct Raw { uint4 v[kHalves][kPanels][2]; };
@@ -162,7 +163,7 @@ struct AttendWarp {
     }
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-    up = 0x1p-126f;
+    up = 0x1p-36f;
   }
 
   // 32 rows from `row` on; k: in shared memory, v: this lane's first piece there; ks, vs: the page's scales, vs in units of `up`, which has
@@ -432,12 +433,12 @@ struct Ring {
     auto drain = [&](int place, int parity) { ring_wait(bar_s + place * 8, parity, limit > kDrainTicks ? limit : kDrainTicks); __syncwarp(); };
     auto use = [&](int x, int place) {
       float shrink = 1.f;
-      if ((x & 31) == 0) {                             // the unit is the largest value scale of all chunks looked up
+      if ((x & 31) == 0) {                             // the unit follows the largest value scale of all chunks looked up
         now = sc;
-        const float top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, x + lane < count ? __float_as_uint(sc.y) : 0u));
-        if (top > w.up) {
-          if (x) shrink = w.up * over(top);
-          w.up = top;
+        const float up = 0x1p-78f * __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, x + lane < count ? __float_as_uint(sc.y) : 0u));
+        if (up > w.up) {
+          if (x) shrink = w.up * over(up);
+          w.up = up;
         }
       }
       const float ks = __shfl_sync(0xFFFFFFFFu, now.x, x & 31), vs = over(w.up) * __shfl_sync(0xFFFFFFFFu, now.y, x & 31);

@@ -178,6 +178,25 @@ def test_attention_over_pages_whose_values_are_far_apart(G, nq):
         c.attend(0, 2, 1, nq, True)
 
 
+@pytest.mark.parametrize("size", [1.0, 1e-6, 1e-13, 1e-22])
+@pytest.mark.parametrize("n", [1, 80])                                       # slices of blocks, of warps
+def test_a_page_of_the_largest_numbers_leaves_other_dims_as_they_are(size, n):
+    """Half of the dims of one page are near the largest numbers, the others 0: what the other pages add there keeps its own precision."""
+    with Both(n_pages=10 * n, n_seqs=n, max_pages=10) as c:
+        v = torch.randn(n, 2, 320, 64, device="cuda") * size
+        for i in range(n):
+            page = 32 * (i % 10)
+            v[i, :, page:page + 32, ::2], v[i, :, page:page + 32, 1::2] = 3e38, 0.0
+        v = v.to(torch.bfloat16)
+        put(c, 0, n, torch.zeros_like(v), v)
+        q, out = torch.zeros(n, 4, 1, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, 4, 1, 64, device="cuda")
+        B.dkv_cache8_attend(c.h, 0, n, 1, q, out)
+        for i in range(n):
+            rows = c.o.rows(i, 1)
+            off = np.abs(out[i, ::2, 0].double().cpu().numpy() - rows.mean(1))
+            assert (off <= 2.0 ** -18 * np.abs(rows).max(1)).all(), i        # of the dim's own largest value: weights all alike
+
+
 def test_many_large_values_whose_logits_pass_the_reference():
     """The first rows of every warp have logits of 0, the others of 6.5 (log2): weights of 2^14.5, of which each warp adds up 960 times
     values near the largest."""
